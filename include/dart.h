@@ -252,7 +252,7 @@ int dart_last_device_status(dart_handle* h, void* cuda_stream);
 int dart_selftest_bounded_wait(dart_handle* h, int32_t spin_limit, int32_t leave_ticket, void* cuda_stream);
 
 /* The cudaError_t (as int) behind the last DART_ERR_CUDA of this handle; with h = NULL, of the last call that has no
- * handle (dart_draft_init, dart_train_attention_fwd, dart_topk_rows_noalloc). */
+ * handle (dart_draft_init, dart_train_attention_fwd, dart_topk_rows_noalloc, dart_kv8_*). */
 int dart_last_cuda_error(const dart_handle* h);
 
 /* Human-readable name of a dart_status. */
@@ -376,6 +376,143 @@ int dart_set_profile_events(dart_handle* h, int stage, void* start_event, void* 
  */
 int dart_topk_rows_noalloc(const float* logits, int32_t rows, int32_t vocab, int32_t topk, float eps_logit,
                            int32_t* out_ids, float* out_slogit, void* cuda_stream);
+
+/*
+ * ---- The target's KV cache in 8 bits, in pages -------------------------------------------------------------------
+ * The draft tree is verified by the target model in one forward pass with tree attention (Section 3, Figure 2).  The
+ * paper leaves the target's cache to its serving stack; these calls are that cache: attention of a step's new rows
+ * (a tree, a prompt's chunk, a single token) over pages of 8-bit keys and values, the append that commits the accepted
+ * rows, and the page operations of a process that serves many sequences.  None needs a handle; nothing is allocated;
+ * everything is asynchronous on `cuda_stream` and may be captured into a CUDA graph (lengths, tables and counts are read
+ * on the DEVICE when the kernels run; the HOST arguments only bound them).
+ *
+ * A page holds `page_tokens` consecutive tokens of one sequence for every layer and KV head.  Value = scale * code,
+ * one fp32 scale per (layer, page, KV head) for keys and one for values: code e4m3 (DART_KV8_E4M3) or a two's-
+ * complement integer -127 .. 127 (DART_KV8_INT8).  Position t of the sequence in slot i is token t % page_tokens of page
+ * page_table[i][t / page_tokens].
+ *
+ * Device-detected errors go to the caller's `status` word (DEVICE i32, may be NULL; never cleared by the calls):
+ * DART_ERR_INVALID_ARG for a length, count, slot or page id out of its bounds (the sequence's outputs are then void,
+ * nothing outside the buffers is touched), DART_ERR_CAPACITY for a pool without enough free pages, DART_ERR_TIMEOUT
+ * for a bounded wait that ran out.
+ */
+#define DART_KV8_E4M3 0
+#define DART_KV8_INT8 1
+typedef struct dart_kv8_cache {
+  int32_t format;        /* DART_KV8_E4M3 or DART_KV8_INT8 */
+  int32_t n_layers;      /* 1..1024 */
+  int32_t n_pages;       /* 1..2^24 */
+  int32_t n_kv_heads;    /* 1..256 */
+  int32_t page_tokens;   /* 16, 32, 64 or 128 */
+  int32_t head_dim;      /* 64 or 128 */
+  void* k_pages;         /* DEVICE u8  [n_layers, n_pages, n_kv_heads, page_tokens, head_dim], 16-byte aligned */
+  void* v_pages;         /* DEVICE u8, same layout */
+  float* k_scale;        /* DEVICE f32 [n_layers, n_pages, n_kv_heads]; positive and finite for pages in use */
+  float* v_scale;        /* DEVICE f32, same layout */
+} dart_kv8_cache;
+
+/*
+ * Attention of `rows` new rows per sequence over the cache and over each other.  Row r of batch entry b sits in sequence
+ * slot slots[b] (or b), reads the slot's seq_lens cached positions and the new rows y <= r (mask == NULL) or those with
+ * mask[b][r][y] != 0 (a draft tree's attention mask as dart_build_tree writes it, self included); new rows from
+ * n_rows[b] on do not exist.  Without k_new / v_new the rows read the cache alone.  Grouped-query heads: head j reads KV
+ * head j / (n_q_heads / n_kv_heads).  Softmax scale 1 / sqrt(head_dim), keys post-RoPE.  Every row of `out` is written;
+ * rows that see no key and rows from n_rows[b] on are zero.  What hidden rows, rows that do not exist and positions
+ * behind a sequence's length hold (infinities and NaN included) does not reach the output.
+ */
+typedef struct dart_kv8_attn_in {
+  int32_t layer;
+  int32_t batch;             /* 1..1024 */
+  int32_t rows;              /* R: 1..4096; with a mask 1..64 */
+  int32_t n_q_heads;         /* a multiple of n_kv_heads, at most 128 per KV head */
+  int32_t max_seqs;          /* rows of page_table and seq_lens; >= batch without slots */
+  int32_t max_pages;         /* columns of page_table */
+  int32_t max_len;           /* HOST bound of seq_lens, 0 .. max_pages * page_tokens: sizes the launch and the workspace */
+  const void* q;             /* DEVICE bf16 [batch, R, n_q_heads, head_dim], RoPE applied */
+  const void* k_new;         /* DEVICE bf16 [batch, R, n_kv_heads, head_dim] or NULL (then v_new and mask are NULL too) */
+  const void* v_new;
+  int64_t q_stride;          /* elements from one row to the next, >= n_q_heads * head_dim, a multiple of 8; entries of
+                                the batch are R rows apart (so q, k_new, v_new may be slices of one QKV matrix) */
+  int64_t new_stride;        /* the same for k_new and v_new, >= n_kv_heads * head_dim */
+  const int32_t* slots;      /* DEVICE i32 [batch] or NULL (slot b) */
+  const int32_t* seq_lens;   /* DEVICE i32 [max_seqs] */
+  const int32_t* page_table; /* DEVICE i32 [max_seqs, max_pages] */
+  const int32_t* n_rows;     /* DEVICE i32 [batch], 0..R, or NULL (R) */
+  const uint8_t* mask;       /* DEVICE u8 [batch, R, R] or NULL (causal) */
+  void* out;                 /* DEVICE bf16 [batch, R, n_q_heads, head_dim] */
+  void* workspace;           /* DEVICE, 16-byte aligned, dart_kv8_attention_workspace_bytes; calls that may overlap (other
+                                streams, other graphs) need one each */
+  size_t workspace_bytes;
+  int32_t* status;
+} dart_kv8_attn_in;
+int dart_kv8_attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, void* cuda_stream);
+/* Workspace for this shape and any smaller max_len; 0 for arguments dart_kv8_attention refuses. */
+size_t dart_kv8_attention_workspace_bytes(const dart_kv8_cache* cache, int32_t batch, int32_t rows, int32_t n_q_heads, int32_t max_len);
+
+/*
+ * Append: row j < n_append[b] of batch entry b -- source row row_index[b][j] of k_new / v_new, or row j -- goes to position
+ * seq_lens + j of its slot, for layers first_layer .. first_layer + n_layers - 1 at once.  After a verification the
+ * source rows are the accepted path: row_index = its row of dart_verify_out.retrieve.  The pages must be the sequence's
+ * own (dart_kv8_reserve); the caller advances seq_lens afterwards.
+ * Scale of a page and head: the smallest power of two s >= 2^-64 with |x| <= qmax * s (qmax 448 or 127) over the finite
+ * new values that the call writes there, or the page's scale if the sequence already has rows in it and that is larger;
+ * codes are x / s rounded to nearest even (exact division, one rounding).  A scale that grows re-rounds the page's
+ * older codes to it.  Infinities become the largest code; NaN becomes e4m3's NaN, or 0 in int8.
+ * A slot that appears twice in `slots` is written once (the first time) and reported.
+ */
+typedef struct dart_kv8_append_in {
+  int32_t first_layer, n_layers;
+  int32_t batch;             /* 1..1024 */
+  int32_t rows;              /* R: source rows per batch entry, 1..2^20 */
+  int32_t max_append;        /* HOST bound of n_append, 1..2^20 (<= R without row_index); columns of row_index */
+  int32_t max_seqs, max_pages;
+  const void* k_new;         /* DEVICE bf16 [n_layers, batch, R, n_kv_heads, head_dim] */
+  const void* v_new;
+  int64_t row_stride;        /* elements from one row to the next, a multiple of 8; batch entries are R rows apart */
+  int64_t layer_stride;      /* elements from one layer to the next, a multiple of 8 */
+  const int32_t* slots;      /* DEVICE i32 [batch] or NULL */
+  const int32_t* seq_lens;   /* DEVICE i32 [max_seqs] */
+  const int32_t* page_table; /* DEVICE i32 [max_seqs, max_pages] */
+  const int32_t* n_append;   /* DEVICE i32 [batch], 0..max_append, or NULL (max_append) */
+  const int32_t* row_index;  /* DEVICE i32 [batch, max_append], entries 0..R-1, or NULL */
+  int32_t* status;
+} dart_kv8_append_in;
+int dart_kv8_append(const dart_kv8_cache* cache, const dart_kv8_append_in* in, void* cuda_stream);
+
+/*
+ * Bookkeeping of a pool: which pages each sequence slot holds, and how many table entries name each page (0: free).
+ * All three arrays are the caller's; a pool starts with table -1, lengths 0, counts 0.  Sequences share pages after a
+ * fork; a shared page is never written (reserve replaces it first).  Lists name slots; a slot or pair that is out of
+ * range, named twice, or (fork) has a source that is also a destination or a destination in use, is skipped and reported.
+ */
+typedef struct dart_kv8_pages {
+  int32_t n_pages, page_tokens;
+  int32_t max_seqs;          /* 1..65536 */
+  int32_t max_pages;
+  int32_t* page_table;       /* DEVICE i32 [max_seqs, max_pages], -1 = no page */
+  int32_t* seq_lens;         /* DEVICE i32 [max_seqs] */
+  int32_t* ref_count;        /* DEVICE i32 [n_pages] */
+} dart_kv8_pages;
+/* Slot dst[i] becomes a copy of slot src[i] (length, and the pages that hold its tokens, shared).  n: 1..1024 pairs. */
+int dart_kv8_fork(const dart_kv8_pages* pages, const int32_t* src, const int32_t* dst, int32_t n, int32_t* status, void* cuda_stream);
+/*
+ * Makes positions seq_len .. seq_len + n_new[i] - 1 of the slots seqs[i] writable: missing pages are taken from the free
+ * ones (lowest ids first, in list order), a page in that range that other slots share is replaced by a copy of all
+ * layers (when every slot that shares it is listed, the last one keeps it).  seq_lens stay.  All or nothing: without
+ * enough free pages nothing changes and the status is DART_ERR_CAPACITY.  n: 1..1024.
+ */
+int dart_kv8_reserve(const dart_kv8_pages* pages, const dart_kv8_cache* cache, const int32_t* seqs, const int32_t* n_new, int32_t n,
+                     void* workspace, size_t workspace_bytes, int32_t* status, void* cuda_stream);
+/* The slots give back all their pages; a page that nobody else names is free again.  n: 1..1024. */
+int dart_kv8_release(const dart_kv8_pages* pages, const int32_t* seqs, int32_t n, int32_t* status, void* cuda_stream);
+/*
+ * Moves the pages in use to the front of the pool: with n_live pages in use, those with ids >= n_live go to the free ids
+ * below n_live (ascending to ascending; all layers), and tables and counts follow.  n_live_out: DEVICE i32 or NULL.
+ */
+int dart_kv8_compact(const dart_kv8_pages* pages, const dart_kv8_cache* cache, int32_t* n_live_out, void* workspace, size_t workspace_bytes,
+                     int32_t* status, void* cuda_stream);
+/* Workspace of reserve and compact (16-byte aligned; one call at a time). */
+size_t dart_kv8_pages_workspace_bytes(const dart_kv8_pages* pages);
 
 #ifdef __cplusplus
 }

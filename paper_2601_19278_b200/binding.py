@@ -29,6 +29,8 @@ EXPORTS = [
     "dart_draft_init", "dart_draft_step", "dart_build_tree", "dart_draft_destroy", "dart_last_device_status",
     "dart_last_cuda_error", "dart_status_string", "dart_workspace_bytes", "dart_ngram_bytes", "dart_train_attention_fwd", "dart_step_launch_count", "dart_draft_prefill", "dart_tree_verify_inputs",
     "dart_set_profile_events", "dart_topk_rows_noalloc", "dart_selftest_bounded_wait", "dart_draft_step_host",
+    "dart_kv8_attention", "dart_kv8_attention_workspace_bytes", "dart_kv8_append", "dart_kv8_fork", "dart_kv8_reserve", "dart_kv8_release",
+    "dart_kv8_compact", "dart_kv8_pages_workspace_bytes",
 ]
 
 
@@ -105,6 +107,35 @@ class DartHostIo(C.Structure):
                 ("out_dev", C.c_void_p), ("out_host", C.c_void_p), ("out_bytes", C.c_size_t)]
 
 
+KV8_E4M3, KV8_INT8 = 0, 1
+
+
+class DartKv8Cache(C.Structure):
+    _fields_ = [("format", C.c_int32), ("n_layers", C.c_int32), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("page_tokens", C.c_int32), ("head_dim", C.c_int32), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class DartKv8AttnIn(C.Structure):
+    _fields_ = [("layer", C.c_int32), ("batch", C.c_int32), ("rows", C.c_int32), ("n_q_heads", C.c_int32), ("max_seqs", C.c_int32),
+                ("max_pages", C.c_int32), ("max_len", C.c_int32), ("q", C.c_void_p), ("k_new", C.c_void_p), ("v_new", C.c_void_p),
+                ("q_stride", C.c_int64), ("new_stride", C.c_int64), ("slots", C.c_void_p), ("seq_lens", C.c_void_p),
+                ("page_table", C.c_void_p), ("n_rows", C.c_void_p), ("mask", C.c_void_p), ("out", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t), ("status", C.c_void_p)]
+
+
+class DartKv8AppendIn(C.Structure):
+    _fields_ = [("first_layer", C.c_int32), ("n_layers", C.c_int32), ("batch", C.c_int32), ("rows", C.c_int32), ("max_append", C.c_int32),
+                ("max_seqs", C.c_int32), ("max_pages", C.c_int32), ("k_new", C.c_void_p), ("v_new", C.c_void_p), ("row_stride", C.c_int64),
+                ("layer_stride", C.c_int64), ("slots", C.c_void_p), ("seq_lens", C.c_void_p), ("page_table", C.c_void_p),
+                ("n_append", C.c_void_p), ("row_index", C.c_void_p), ("status", C.c_void_p)]
+
+
+class DartKv8Pages(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("max_seqs", C.c_int32), ("max_pages", C.c_int32),
+                ("page_table", C.c_void_p), ("seq_lens", C.c_void_p), ("ref_count", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -153,6 +184,18 @@ def lib() -> C.CDLL:
         L.dart_topk_rows_noalloc.restype = C.c_int
         L.dart_selftest_bounded_wait.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]
         L.dart_selftest_bounded_wait.restype = C.c_int
+        P = C.c_void_p
+        L.dart_kv8_attention.argtypes = [P, P, P]
+        L.dart_kv8_attention_workspace_bytes.argtypes = [P, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+        L.dart_kv8_append.argtypes = [P, P, P]
+        L.dart_kv8_fork.argtypes = [P, P, P, C.c_int32, P, P]
+        L.dart_kv8_release.argtypes = [P, P, C.c_int32, P, P]
+        L.dart_kv8_reserve.argtypes = [P, P, P, P, C.c_int32, P, C.c_size_t, P, P]
+        L.dart_kv8_compact.argtypes = [P, P, P, P, C.c_size_t, P, P]
+        L.dart_kv8_pages_workspace_bytes.argtypes = [P]
+        for name in ("attention", "append", "fork", "release", "reserve", "compact"):
+            getattr(L, "dart_kv8_" + name).restype = C.c_int
+        L.dart_kv8_attention_workspace_bytes.restype = L.dart_kv8_pages_workspace_bytes.restype = C.c_size_t
         _lib = L
     return _lib
 
@@ -327,6 +370,196 @@ def train_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_l
     rc = lib().dart_train_attention_fwd(C.byref(a), C.c_void_p(st.cuda_stream))
     if rc != DART_OK:
         raise DartError(rc, "dart_train_attention_fwd", lib().dart_last_cuda_error(None))
+
+
+# ---- the target's KV cache in 8 bits, in pages ------------------------------------------------------------------------
+def _kv8_check(t: Optional[torch.Tensor], name: str, dtype, dev: torch.device, shape=None) -> Optional[int]:
+    """Address of a contiguous tensor of this type, device and shape (None stays None); ValueError otherwise."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor on {dev} is needed, got {t.dtype} on {t.device}"
+                         f"{'' if t.is_contiguous() else ', not contiguous'}")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name}: shape {shape} is needed, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _kv8_rows(t: torch.Tensor, name: str, heads: int, dim: int, dev: torch.device) -> int:
+    """Row stride of bf16 [batch, rows, heads, dim] whose heads are packed and whose batch entries are `rows` rows apart."""
+    if t.dtype != torch.bfloat16 or t.device != dev or t.dim() != 4 or t.shape[2] != heads or t.shape[3] != dim:
+        raise ValueError(f"{name}: bf16 [batch, rows, {heads}, {dim}] on {dev} is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    B, R = t.shape[:2]
+    s0, s1, s2, s3 = t.stride()
+    row = s1 if R > 1 else s0 if B > 1 else heads * dim
+    if s3 != 1 or (heads > 1 and s2 != dim) or (B > 1 and R > 1 and s0 != R * s1):
+        raise ValueError(f"{name}: heads must be packed and batch entries {R} rows apart, got strides {t.stride()}")
+    return row
+
+
+def _kv8_call(fn, name: str, dev: torch.device, stream, *args) -> None:
+    """One call with `dev` current and the stream's handle as its last argument."""
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _kv8_call(fn, name, dev, stream, *args)
+    st = stream if stream is not None else torch.cuda.current_stream(dev)
+    rc = fn(*args, st.cuda_stream)
+    if rc != DART_OK:
+        raise DartError(rc, name, lib().dart_last_cuda_error(None) if rc == DART_ERR_CUDA else 0)
+
+
+class Kv8Cache:
+    """dart_kv8_cache over caller-owned tensors: k_pages, v_pages float8_e4m3fn or int8 [n_layers, n_pages, n_kv_heads,
+    page_tokens, head_dim], k_scale, v_scale fp32 [n_layers, n_pages, n_kv_heads]."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        if k_pages.dtype not in (torch.float8_e4m3fn, torch.int8) or k_pages.dim() != 5:
+            raise ValueError("k_pages: float8_e4m3fn or int8 [n_layers, n_pages, n_kv_heads, page_tokens, head_dim] is needed, got "
+                             f"{k_pages.dtype} {tuple(k_pages.shape)}")
+        if not k_pages.is_cuda:
+            raise ValueError("k_pages must be on a CUDA device (there is no CPU fallback)")
+        self.device = k_pages.device
+        shape = tuple(k_pages.shape)
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = shape
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale    # keep the tensors alive
+        self.c = DartKv8Cache(KV8_E4M3 if k_pages.dtype == torch.float8_e4m3fn else KV8_INT8, *shape,
+                              _kv8_check(k_pages, "k_pages", k_pages.dtype, self.device),
+                              _kv8_check(v_pages, "v_pages", k_pages.dtype, self.device, shape),
+                              _kv8_check(k_scale, "k_scale", torch.float32, self.device, shape[:3]),
+                              _kv8_check(v_scale, "v_scale", torch.float32, self.device, shape[:3]))
+        self.ref = C.addressof(self.c)
+
+
+class Kv8Pages:
+    """dart_kv8_pages over caller-owned int32 tensors: page_table [max_seqs, max_pages], seq_lens [max_seqs], ref_count
+    [n_pages].  A new pool starts with table -1, lengths 0, counts 0."""
+
+    def __init__(self, page_table: torch.Tensor, seq_lens: torch.Tensor, ref_count: torch.Tensor, page_tokens: int):
+        if not page_table.is_cuda:
+            raise ValueError("page_table must be on a CUDA device (there is no CPU fallback)")
+        self.device = page_table.device
+        self.page_table, self.seq_lens, self.ref_count = page_table, seq_lens, ref_count
+        if page_table.dim() != 2 or ref_count.dim() != 1:
+            raise ValueError("page_table [max_seqs, max_pages] and ref_count [n_pages] are needed")
+        S, M = page_table.shape
+        self.c = DartKv8Pages(ref_count.shape[0], page_tokens, S, M, _kv8_check(page_table, "page_table", torch.int32, self.device),
+                              _kv8_check(seq_lens, "seq_lens", torch.int32, self.device, (S,)),
+                              _kv8_check(ref_count, "ref_count", torch.int32, self.device))
+        self.ref = C.addressof(self.c)
+
+
+def kv8_attention_workspace_bytes(cache: Kv8Cache, batch: int, rows: int, n_q_heads: int, max_len: int) -> int:
+    return lib().dart_kv8_attention_workspace_bytes(cache.ref, batch, rows, n_q_heads, max_len)
+
+
+def kv8_attention(cache: Kv8Cache, layer: int, q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: Optional[torch.Tensor],
+                  seq_lens: torch.Tensor, page_table: torch.Tensor, out: torch.Tensor, *, max_len: int, workspace: torch.Tensor,
+                  slots: Optional[torch.Tensor] = None, n_rows: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                  status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dart_kv8_attention: q, out [batch, rows, n_q_heads, head_dim], k_new, v_new [batch, rows, n_kv_heads, head_dim] bf16 (q and the
+    new rows may be slices of one QKV matrix); seq_lens, page_table, slots, n_rows int32 on the device; mask u8
+    [batch, rows, rows] (dart_tree_out.mask) or None: causal.  max_len: host bound of the lengths."""
+    dev = cache.device
+    if q.dim() != 4:
+        raise ValueError(f"q: [batch, rows, n_q_heads, head_dim] is needed, got {tuple(q.shape)}")
+    B, R, H, d = q.shape
+    qs = _kv8_rows(q, "q", H, cache.head_dim, dev)
+    kp = vp = None
+    ns = 0
+    if k_new is not None:
+        if v_new is None or tuple(k_new.shape[:2]) != (B, R) or tuple(v_new.shape[:2]) != (B, R):
+            raise ValueError("k_new and v_new: both [batch, rows, n_kv_heads, head_dim] with q's batch and rows, or neither")
+        ns = _kv8_rows(k_new, "k_new", cache.n_kv_heads, d, dev)
+        if _kv8_rows(v_new, "v_new", cache.n_kv_heads, d, dev) != ns:
+            raise ValueError("k_new and v_new must have the same row stride")
+        kp, vp = k_new.data_ptr(), v_new.data_ptr()
+    elif v_new is not None:
+        raise ValueError("v_new without k_new")
+    if page_table.dim() != 2:
+        raise ValueError("page_table: [max_seqs, max_pages] is needed")
+    S, M = page_table.shape
+    i32 = torch.int32
+    a = DartKv8AttnIn(layer, B, R, H, S, M, max_len, q.data_ptr(), kp, vp, qs, ns, _kv8_check(slots, "slots", i32, dev, (B,)),
+                      _kv8_check(seq_lens, "seq_lens", i32, dev, (S,)), _kv8_check(page_table, "page_table", i32, dev),
+                      _kv8_check(n_rows, "n_rows", i32, dev, (B,)), _kv8_check(mask, "mask", torch.uint8, dev, (B, R, R)),
+                      _kv8_check(out, "out", torch.bfloat16, dev, (B, R, H, d)), _kv8_check(workspace, "workspace", torch.uint8, dev),
+                      workspace.numel(), _kv8_check(status, "status", i32, dev))
+    _kv8_call(lib().dart_kv8_attention, "dart_kv8_attention", dev, stream, cache.ref, C.byref(a))
+
+
+def kv8_append(cache: Kv8Cache, first_layer: int, k_new: torch.Tensor, v_new: torch.Tensor, seq_lens: torch.Tensor,
+               page_table: torch.Tensor, *, n_append: Optional[torch.Tensor] = None, row_index: Optional[torch.Tensor] = None,
+               max_append: Optional[int] = None, slots: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+               stream=None) -> None:
+    """dart_kv8_append: k_new, v_new bf16 [n_layers, batch, rows, n_kv_heads, head_dim]; row_index int32 [batch, max_append] (an
+    accepted path of dart_tree_verify_inputs) or None: the rows in order.  The caller advances seq_lens."""
+    dev = cache.device
+    if k_new.dim() != 5 or tuple(v_new.shape) != tuple(k_new.shape):
+        raise ValueError("k_new and v_new: [n_layers, batch, rows, n_kv_heads, head_dim] are needed, of one shape")
+    L, B, R = k_new.shape[:3]
+    if L < 1:
+        raise ValueError("k_new: at least one layer is needed")
+    rs = _kv8_rows(k_new[0], "k_new", cache.n_kv_heads, cache.head_dim, dev)
+    ls = k_new.stride(0) if L > 1 else 0
+    if _kv8_rows(v_new[0], "v_new", cache.n_kv_heads, cache.head_dim, dev) != rs or (L > 1 and v_new.stride(0) != ls):
+        raise ValueError("k_new and v_new must have the same strides")
+    if page_table.dim() != 2:
+        raise ValueError("page_table: [max_seqs, max_pages] is needed")
+    A = max_append if max_append is not None else row_index.shape[1] if row_index is not None else R
+    S, M = page_table.shape
+    i32 = torch.int32
+    a = DartKv8AppendIn(first_layer, L, B, R, A, S, M, k_new.data_ptr(), v_new.data_ptr(), rs, ls, _kv8_check(slots, "slots", i32, dev, (B,)),
+                        _kv8_check(seq_lens, "seq_lens", i32, dev, (S,)), _kv8_check(page_table, "page_table", i32, dev),
+                        _kv8_check(n_append, "n_append", i32, dev, (B,)), _kv8_check(row_index, "row_index", i32, dev, (B, A)),
+                        _kv8_check(status, "status", i32, dev))
+    _kv8_call(lib().dart_kv8_append, "dart_kv8_append", dev, stream, cache.ref, C.byref(a))
+
+
+def kv8_pages_workspace_bytes(pages: Kv8Pages) -> int:
+    return lib().dart_kv8_pages_workspace_bytes(pages.ref)
+
+
+def _kv8_lists(dev: torch.device, **lists: torch.Tensor):
+    n = next(iter(lists.values())).numel()
+    return [_kv8_check(t, name, torch.int32, dev, (n,)) for name, t in lists.items()] + [n]
+
+
+def kv8_fork(pages: Kv8Pages, src: torch.Tensor, dst: torch.Tensor, *, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dart_kv8_fork: slot dst[i] becomes a copy of slot src[i] (shared pages)."""
+    sp, dp, n = _kv8_lists(pages.device, src=src, dst=dst)
+    _kv8_call(lib().dart_kv8_fork, "dart_kv8_fork", pages.device, stream, pages.ref, sp, dp, n,
+              _kv8_check(status, "status", torch.int32, pages.device))
+
+
+def kv8_release(pages: Kv8Pages, seqs: torch.Tensor, *, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dart_kv8_release: the slots give back all their pages."""
+    sp, n = _kv8_lists(pages.device, seqs=seqs)
+    _kv8_call(lib().dart_kv8_release, "dart_kv8_release", pages.device, stream, pages.ref, sp, n,
+              _kv8_check(status, "status", torch.int32, pages.device))
+
+
+def _kv8_same_pool(pages: Kv8Pages, cache: Kv8Cache) -> None:
+    if cache.device != pages.device:
+        raise ValueError("the cache and its bookkeeping must be on one device")
+
+
+def kv8_reserve(pages: Kv8Pages, cache: Kv8Cache, seqs: torch.Tensor, n_new: torch.Tensor, *, workspace: torch.Tensor,
+                status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dart_kv8_reserve: pages for the next n_new[i] positions of slot seqs[i]; shared ones are replaced by copies."""
+    _kv8_same_pool(pages, cache)
+    sp, np_, n = _kv8_lists(pages.device, seqs=seqs, n_new=n_new)
+    _kv8_call(lib().dart_kv8_reserve, "dart_kv8_reserve", pages.device, stream, pages.ref, cache.ref, sp, np_, n,
+              _kv8_check(workspace, "workspace", torch.uint8, pages.device), workspace.numel(),
+              _kv8_check(status, "status", torch.int32, pages.device))
+
+
+def kv8_compact(pages: Kv8Pages, cache: Kv8Cache, *, workspace: torch.Tensor, n_live: Optional[torch.Tensor] = None,
+                status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dart_kv8_compact: the pages in use move to the front of the pool."""
+    _kv8_same_pool(pages, cache)
+    _kv8_call(lib().dart_kv8_compact, "dart_kv8_compact", pages.device, stream, pages.ref, cache.ref,
+              _kv8_check(n_live, "n_live", torch.int32, pages.device), _kv8_check(workspace, "workspace", torch.uint8, pages.device),
+              workspace.numel(), _kv8_check(status, "status", torch.int32, pages.device))
 
 
 def workspace_bytes(cfg: DartConfig) -> int:

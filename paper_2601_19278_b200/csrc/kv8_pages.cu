@@ -1,0 +1,293 @@
+// Pages of the 8-bit cache: fork, reserve with copy-on-write, release, compact.
+//
+// The one truth about a page is its reference count (0: free); there is no free list to keep consistent.  Pages are
+// handed out lowest id first, in list order, so that two runs of the same calls give the same tables.  Reserve and
+// compact are a planning kernel of one block (prefix sums over the counts; a few microseconds) that leaves a list of
+// (source, destination) pages in the workspace, and a copy kernel over the list, whose length only the device knows.
+#include "kv8.cuh"
+
+namespace dart {
+
+constexpr int kPgThreads = 1024;
+// Workspace, in ints: [0] entries of the copy list; [16..]: destinations, sources (-1: nothing to copy), slots, columns;
+// compact uses the third array for the new ids.
+constexpr int kPgHead = 16;
+size_t kv8_pages_workspace(int n_pages) { return ((size_t)kPgHead + 4 * (size_t)n_pages) * sizeof(int); }
+
+// Exclusive prefix sum of v over the block's threads; *total gets the sum.  sh: 33 ints; the caller syncs before reuse.
+__device__ __forceinline__ int block_scan(int v, int* sh, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) sh[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    const int s = lane < (int)(blockDim.x >> 5) ? sh[lane] : 0;
+    int t = s;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, t, o);
+      if (lane >= o) t += y;
+    }
+    sh[lane] = t - s;
+    if (lane == 31) sh[32] = t;
+  }
+  __syncthreads();
+  *total = sh[32];
+  return sh[warp] + x - v;
+}
+
+__global__ void __launch_bounds__(256) kv8_fork_kernel(const Kv8PagesArgs p, const int* src, const int* dst, int n, int* status) {
+  const int i = blockIdx.x, tid = threadIdx.x;
+  const int s = src[i], d = dst[i];
+  int bad = s < 0 || s >= p.max_seqs || d < 0 || d >= p.max_seqs || s == d;
+  for (int t = tid; t < n; t += blockDim.x) bad |= dst[t] == s || (t < i && dst[t] == d);
+  int len = 0;
+  if (!bad) {      // slot s is nobody's destination, so no block of this call writes it
+    len = p.seq_lens[s];
+    bad = len < 0 || (long long)len > (long long)p.max_pages * p.pt || p.seq_lens[d] != 0;
+    for (int j = tid; j < p.max_pages; j += blockDim.x) bad |= p.table[(size_t)d * p.max_pages + j] != -1;
+  }
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) kv8_report(status, KV8_BAD_ARG);
+    return;
+  }
+  const int cols = (len + p.pt - 1) / p.pt;
+  for (int j = tid; j < cols; j += blockDim.x) {
+    const int e = p.table[(size_t)s * p.max_pages + j];
+    if (e < 0 || e >= p.n_pages) { kv8_report(status, KV8_BAD_ARG); continue; }
+    p.table[(size_t)d * p.max_pages + j] = e;
+    atomicAdd(&p.ref[e], 1);
+  }
+  if (tid == 0) p.seq_lens[d] = len;
+}
+
+__global__ void __launch_bounds__(256) kv8_release_kernel(const Kv8PagesArgs p, const int* seqs, int* status) {
+  const int i = blockIdx.x, tid = threadIdx.x, s = seqs[i];
+  int bad = s < 0 || s >= p.max_seqs;
+  for (int t = tid; t < i; t += blockDim.x) bad |= seqs[t] == s;
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) kv8_report(status, KV8_BAD_ARG);
+    return;
+  }
+  for (int j = tid; j < p.max_pages; j += blockDim.x) {
+    int* e = p.table + (size_t)s * p.max_pages + j;
+    const int page = *e;
+    if (page == -1) continue;
+    *e = -1;
+    if (page < 0 || page >= p.n_pages) { kv8_report(status, KV8_BAD_ARG); continue; }
+    if (atomicSub(&p.ref[page], 1) <= 0) { atomicAdd(&p.ref[page], 1); kv8_report(status, KV8_BAD_ARG); }
+  }
+  if (tid == 0) p.seq_lens[s] = 0;
+}
+
+__global__ void __launch_bounds__(kPgThreads) kv8_reserve_plan_kernel(const Kv8PagesArgs p, const int* seqs, const int* n_new, int n, int* ws,
+                                                                      int* status) {
+  __shared__ int sh[33], s_slot[kPgThreads], s_lo[kPgThreads], s_start[kPgThreads + 1];
+  const int tid = threadIdx.x;
+  int* dst = ws + kPgHead;
+  int *src = dst + p.n_pages, *slot = src + p.n_pages, *column = slot + p.n_pages;
+  // the columns [lo, lo + width) that item tid wants to write
+  s_slot[tid] = tid < n ? seqs[tid] : -1;
+  __syncthreads();
+  int width = 0, lo = 0;
+  if (tid < n) {
+    const int s = s_slot[tid], m = n_new[tid];
+    bool bad = s < 0 || s >= p.max_seqs || m < 0;
+    for (int t = 0; t < tid; ++t) bad |= s_slot[t] == s;
+    const int len = bad ? 0 : p.seq_lens[s];
+    if (len < 0 || (!bad && (long long)len + m > (long long)p.max_pages * p.pt)) bad = true;
+    if (bad) kv8_report(status, KV8_BAD_ARG);
+    else if (m > 0) { lo = len / p.pt; width = (len + m - 1) / p.pt + 1 - lo; }
+  }
+  s_lo[tid] = lo;
+  int total_cols, total_need = 0;
+  const int start = block_scan(width, sh, &total_cols);
+  s_start[tid] = start;
+  if (tid == 0) s_start[kPgThreads] = total_cols;
+  __syncthreads();
+  // (item, column) pairs in list order: which need a page
+  for (int base = 0; base < total_cols; base += kPgThreads) {
+    const int f = base + tid;
+    int need = 0, old = -1, s = 0, j = 0;
+    if (f < total_cols) {
+      int a = 0, b = kPgThreads - 1;             // the last item that starts at or before f
+      while (a < b) {
+        const int c = (a + b + 1) >> 1;
+        if (s_start[c] <= f) a = c; else b = c - 1;
+      }
+      s = s_slot[a];
+      j = s_lo[a] + f - s_start[a];
+      const int e = p.table[(size_t)s * p.max_pages + j];
+      if (e == -1) need = 1;
+      else if (e < 0 || e >= p.n_pages) kv8_report(status, KV8_BAD_ARG);
+      else if (p.ref[e] > 1) {                   // shared: earlier items of the list copy first, the last sharer keeps it
+        int rank = 0;
+        for (int t = 0; t < a; ++t)
+          if (s_start[t + 1] > s_start[t] && j >= s_lo[t] && j < s_lo[t] + s_start[t + 1] - s_start[t])
+            rank += p.table[(size_t)s_slot[t] * p.max_pages + j] == e;
+        if (rank < p.ref[e] - 1) { need = 1; old = e; }
+      }
+    }
+    int here;
+    const int k = total_need + block_scan(need, sh, &here);
+    if (need && k < p.n_pages) { src[k] = old; slot[k] = s; column[k] = j; }
+    total_need += here;
+  }
+  __syncthreads();
+  // the lowest free pages
+  int found = 0;
+  for (int base = 0; base < p.n_pages && found < total_need; base += 4 * kPgThreads) {
+    int free_bits = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int id = base + tid * 4 + q;
+      if (id < p.n_pages && p.ref[id] == 0) free_bits |= 1 << q;
+    }
+    int here;
+    int k = found + block_scan(__popc(free_bits), sh, &here);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if ((free_bits >> q) & 1) {
+        if (k < total_need) dst[k] = base + tid * 4 + q;
+        ++k;
+      }
+    found += here;
+  }
+  __syncthreads();
+  const bool ok = found >= total_need;
+  if (ok)
+    for (int k = tid; k < total_need; k += kPgThreads) {
+      const int page = dst[k];
+      p.table[(size_t)slot[k] * p.max_pages + column[k]] = page;
+      p.ref[page] = 1;
+      if (src[k] >= 0) atomicSub(&p.ref[src[k]], 1);
+    }
+  if (tid == 0) {
+    ws[0] = ok ? total_need : 0;
+    if (!ok) kv8_report(status, KV8_CAPACITY);
+  }
+}
+
+__global__ void __launch_bounds__(kPgThreads) kv8_compact_plan_kernel(const Kv8PagesArgs p, int* ws, int* n_live_out) {
+  __shared__ int sh[33];
+  const int tid = threadIdx.x;
+  int* dst = ws + kPgHead;
+  int *src = dst + p.n_pages, *to = src + p.n_pages;
+  int mine = 0, n_live;
+  for (int id = tid; id < p.n_pages; id += kPgThreads) mine += p.ref[id] > 0;
+  block_scan(mine, sh, &n_live);
+  int n_src = 0, n_dst = 0;      // as many live pages at n_live and above as free ones below it
+  for (int base = 0; base < p.n_pages; base += 4 * kPgThreads) {
+    int moves = 0, holes = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int id = base + tid * 4 + q;
+      if (id >= p.n_pages) continue;
+      to[id] = id;
+      const bool live = p.ref[id] > 0;
+      if (live && id >= n_live) moves |= 1 << q;
+      if (!live && id < n_live) holes |= 1 << q;
+    }
+    int here_src, here_dst;
+    int ks = n_src + block_scan(__popc(moves), sh, &here_src), kd = n_dst + block_scan(__popc(holes), sh, &here_dst);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int id = base + tid * 4 + q;
+      if ((moves >> q) & 1) src[ks++] = id;
+      if ((holes >> q) & 1) dst[kd++] = id;
+    }
+    n_src += here_src;
+    n_dst += here_dst;
+  }
+  __syncthreads();
+  for (int k = tid; k < n_src; k += kPgThreads) {
+    const int s = src[k], d = dst[k];
+    to[s] = d;
+    p.ref[d] = p.ref[s];
+    p.ref[s] = 0;
+  }
+  if (tid == 0) {
+    ws[0] = n_src;
+    if (n_live_out != nullptr) *n_live_out = n_live;
+  }
+}
+
+// Copies the listed pages of every layer, and (compact) renames the table's entries.
+constexpr int kCpThreads = 256, kCpChunk = kCpThreads * 64;   // bytes a block copies at a time
+__global__ void __launch_bounds__(kCpThreads) kv8_copy_pages_kernel(const Kv8PagesArgs p, const Kv8PoolArgs c, const int* ws, int rename) {
+  const int tid = threadIdx.x, count = ws[0];
+  const int* dst = ws + kPgHead;
+  const int *src = dst + p.n_pages, *to = src + p.n_pages;
+  if (rename) {
+    const long long cells = (long long)p.max_seqs * p.max_pages;
+    for (long long i = (long long)blockIdx.x * kCpThreads + tid; i < cells; i += (long long)gridDim.x * kCpThreads) {
+      const int e = p.table[i];
+      if (e >= 0 && e < p.n_pages && to[e] != e) p.table[i] = to[e];
+    }
+  }
+  const int parts = (int)((c.slab + kCpChunk - 1) / kCpChunk);
+  const long long units = (long long)count * c.n_layers * 2 * parts;
+  for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+    long long x = u;
+    const int part = (int)(x % parts); x /= parts;
+    const int is_v = (int)(x & 1); x >>= 1;
+    const int layer = (int)(x % c.n_layers), k = (int)(x / c.n_layers);
+    const int s = src[k], d = dst[k];
+    if (s < 0) continue;
+    const size_t sp = (size_t)layer * c.n_pages + s, dp = (size_t)layer * c.n_pages + d;
+    uint8_t* pool = is_v ? c.v : c.k;
+    const uint4* from = reinterpret_cast<const uint4*>(pool + sp * c.slab);
+    uint4* into = reinterpret_cast<uint4*>(pool + dp * c.slab);
+    const int n16 = (int)(c.slab / 16), at = part * (kCpChunk / 16) + tid;
+    uint4 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (at + q * kCpThreads < n16) v[q] = from[at + q * kCpThreads];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (at + q * kCpThreads < n16) into[at + q * kCpThreads] = v[q];
+    if (part == 0) {
+      float* sc = is_v ? c.vs : c.ks;
+      for (int h = tid; h < c.hkv; h += kCpThreads) sc[dp * c.hkv + h] = sc[sp * c.hkv + h];
+    }
+  }
+}
+
+cudaError_t launch_kv8_fork(const Kv8PagesArgs& p, const int* src, const int* dst, int n, int* status, cudaStream_t st) {
+  kv8_fork_kernel<<<n, 256, 0, st>>>(p, src, dst, n, status);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv8_release(const Kv8PagesArgs& p, const int* seqs, int n, int* status, cudaStream_t st) {
+  kv8_release_kernel<<<n, 256, 0, st>>>(p, seqs, status);
+  return cudaGetLastError();
+}
+
+namespace {
+constexpr int kCpGrid = 148 * 8;
+}
+cudaError_t launch_kv8_reserve(const Kv8PagesArgs& p, const Kv8PoolArgs& c, const int* seqs, const int* n_new, int n, int* ws, int* status,
+                               cudaStream_t st) {
+  kv8_reserve_plan_kernel<<<1, kPgThreads, 0, st>>>(p, seqs, n_new, n, ws, status);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  kv8_copy_pages_kernel<<<kCpGrid, kCpThreads, 0, st>>>(p, c, ws, 0);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv8_compact(const Kv8PagesArgs& p, const Kv8PoolArgs& c, int* n_live, int* ws, int* status, cudaStream_t st) {
+  (void)status;
+  kv8_compact_plan_kernel<<<1, kPgThreads, 0, st>>>(p, ws, n_live);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  kv8_copy_pages_kernel<<<kCpGrid, kCpThreads, 0, st>>>(p, c, ws, 1);
+  return cudaGetLastError();
+}
+
+}  // namespace dart
