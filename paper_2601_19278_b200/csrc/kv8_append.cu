@@ -9,9 +9,6 @@
 
 namespace dart {
 
-// 2^k, -126 <= k <= 127
-__device__ __forceinline__ float pow2i(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
-
 // Exponent of the smallest power of two s >= 2^-64 with value <= qmax * s; `bits`: the value's bf16 bits (finite, >= 0).
 __device__ __forceinline__ int kv8_scale_exp(uint32_t bits, int format) {
   const int E = (int)(bits >> 7), M = (int)(bits & 127);
@@ -96,7 +93,7 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
 #pragma unroll
     for (int i = 0; i < kApThreads / 32; ++i) big = max(big, sh_max[i]);
     const int k = kv8_scale_exp(big, a.format);
-    const float need = pow2i(k), s = fmaxf(need, was);
+    const float need = kv8_pow2(k), s = fmaxf(need, was);
     const bool exact = s == need || (__float_as_uint(s) & 0x7fffffu) == 0u;    // a power of two: the reciprocal is exact
     const float inv = 1.f / s;
 #pragma unroll
