@@ -377,47 +377,69 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
 }
 
 // ---- the join ---------------------------------------------------------------------------------------------------------
-// One warp per row; partials in chunk order.  Sequences that fit one chunk were finished by their only CTA.
+// WPR warps per row, partials in a fixed order.  Sequences that fit one chunk were finished by their only CTA.  What bounds
+// it is one row's chain of reads: with 54 partials a single warp took 38 us, eight warps take @CMB.
+template <int WPR>
 __global__ void __launch_bounds__(256) kv8_combine_kernel(const __grid_constant__ Kv8AttnArgs a, const Kv8Plan plan) {
+  constexpr int kRows = 8 / WPR;
+  __shared__ float s_M[8], s_L[8];
+  __shared__ __align__(16) float4 s_o[8][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, dh = a.c.dh;
-  const int i = blockIdx.x * 8 + warp, h = blockIdx.y, b = blockIdx.z;
+  const int i = blockIdx.x * kRows + warp / WPR, w = warp % WPR, h = blockIdx.y, b = blockIdx.z;
   const Kv8Seq s = kv8_seq(a, b, false);
   const int N = a.rows * a.G, Nv = s.rows * a.G;
-  pdl_wait();
-  if (i >= N) return;
-  int n;
-  size_t part0, step;
-  if (plan.umma) {
-    const int tile = i >> 7;
-    const Kv8Tiles tl = kv8_tiles(a, plan, s, tile);
-    n = tl.split.n;
-    part0 = ((size_t)((b * a.c.hkv + h) * plan.n_tiles + tile) * plan.max_chunks) * 128 + (i & 127);
-    step = 128;
-  } else {
-    n = kv8_split_keys(s.len, plan.chunk).n;
-    part0 = ((size_t)(b * a.c.hkv + h) * plan.max_chunks) * 16 + i;
-    step = 16;
+  int n = 0;
+  size_t part0 = 0, step = 16;
+  if (i < N) {
+    if (plan.umma) {
+      const int tile = i >> 7;
+      n = kv8_tiles(a, plan, s, tile).split.n;
+      part0 = ((size_t)((b * a.c.hkv + h) * plan.n_tiles + tile) * plan.max_chunks) * 128 + (i & 127);
+      step = 128;
+    } else {
+      n = kv8_split_keys(s.len, plan.chunk).n;
+      part0 = ((size_t)(b * a.c.hkv + h) * plan.max_chunks) * 16 + i;
+    }
   }
-  if (n <= 1) return;
-  float M = -INFINITY;
-  for (int c = lane; c < n; c += 32) M = fmaxf(M, plan.ml_part[(part0 + c * step) * 2]);
-  M = warp_max(M);
-  float L = 0.f;
+  pdl_wait();
+  if (WPR == 1 ? n <= 1 : false) return;
+  float M = -INFINITY, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int c4 = lane;      // float4 of the row
+  if (n > 1) {
+    for (int c = w + lane * WPR; c < n; c += 32 * WPR) M = fmaxf(M, plan.ml_part[(part0 + c * step) * 2]);
+    M = warp_max(M);
+    const int c4 = min(lane, dh / 4 - 1);
 #pragma unroll 4
-  for (int c = 0; c < n; ++c) {
-    const size_t p = part0 + c * step;
-    const float2 ml = *reinterpret_cast<const float2*>(plan.ml_part + p * 2);
-    if (ml.y == 0.f) continue;
-    const float f = exp2f(ml.x - M);
-    L += ml.y * f;
-    if (c4 * 4 < dh) {
+    for (int c = w; c < n; c += WPR) {
+      const size_t p = part0 + c * step;
+      const float2 ml = *reinterpret_cast<const float2*>(plan.ml_part + p * 2);
       const float4 v = *reinterpret_cast<const float4*>(plan.o_part + p * dh + c4 * 4);
+      if (ml.y == 0.f) continue;      // no key in this chunk
+      const float f = exp2f(ml.x - M);
+      L += ml.y * f;
       acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
     }
   }
-  if (c4 * 4 < dh) kv8_store_row(a, b, h, i, i < Nv, L, c4, acc);
+  if (WPR > 1) {
+    if (lane == 0) { s_M[warp] = M; s_L[warp] = L; }
+    s_o[warp][lane] = acc;
+    __syncthreads();
+    if (w != 0 || n <= 1) return;
+    M = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < WPR; ++q) M = fmaxf(M, s_M[q]);
+    L = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int q = 0; q < WPR; ++q) {
+      if (s_L[q] == 0.f) continue;
+      const float f = exp2f(s_M[q] - M);
+      const float4 v = s_o[q][lane];
+      L += s_L[q] * f;
+      acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+    }
+  }
+  if (lane * 4 < dh) kv8_store_row(a, b, h, i, i < Nv, L, lane, acc);
 }
 
 // ---- planning ---------------------------------------------------------------------------------------------------------
@@ -486,7 +508,10 @@ cudaError_t launch_kv8_attention(const Kv8AttnArgs& a, void* workspace, cudaStre
   else
     e = a.c.dh == 128 ? launch_stream_rows<KV8_INT8, 128>(a, p, st) : launch_stream_rows<KV8_INT8, 64>(a, p, st);
   if (e != cudaSuccess || p.max_chunks == 1) return e;
-  return launch_pdl(kv8_combine_kernel, dim3((a.rows * a.G + 7) / 8, a.c.hkv, a.batch), dim3(256), 0, st, a, p);
+  const int rows = a.rows * a.G;
+  // eight warps a row where there are few rows and many partials; elsewhere the rows fill the GPU by themselves
+  if (p.max_chunks > 4 && (long long)rows * a.c.hkv * a.batch <= 148 * 8) return launch_pdl(kv8_combine_kernel<8>, dim3(rows, a.c.hkv, a.batch), dim3(256), 0, st, a, p);
+  return launch_pdl(kv8_combine_kernel<1>, dim3((rows + 7) / 8, a.c.hkv, a.batch), dim3(256), 0, st, a, p);
 }
 
 }  // namespace dart
