@@ -26,16 +26,60 @@ namespace dart {
 
 using namespace umma;
 
-constexpr int kKuThreads = 512;      // warps 0: producer, 1 and 3: MMA issuers, 2: tensor memory; 4-7, 8-11: softmax; 12-15: converters
-constexpr int kKuPairSlots = 3, kKuSingleSlots = 7;     // 64-key code slots: what shared memory leaves
+constexpr int kKuThreads = 640;      // warps 0: producer of K, 1 and 3: MMA issuers, 2: producer of V; 4-7, 8-11: softmax; 12-15, 16-19: converters
+constexpr int kKuPairSlots = 2, kKuSingleSlots = 3;     // 64-key code slots of each ring (K, V): what shared memory leaves
 constexpr int kKuBad = 4096 / 32;
 
+#ifndef KU_RELAX_NS
+#define KU_RELAX_NS 64
+#endif
+#ifndef KU_ISSUE_NS
+#define KU_ISSUE_NS 20
+#endif
+// Bounded wait in little code (the loop is not unrolled: there are some twenty of them); about a second, then the CTA's
+// abort flag is raised and all roles leave.
+__device__ __forceinline__ bool ku_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+#pragma unroll 1
+  for (int it = 0; it < 16000000; ++it) {
+    if (mbar_test_wait(bar, parity)) return true;
+    if (*abort_flag) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+
+// The same for the roles that run ahead of the arithmetic: a pause between two looks.  (Twelve warps that polled without one
+// doubled the time of the softmax warps beside them.)
+__device__ __forceinline__ bool ku_wait_relaxed(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+#pragma unroll 1
+  for (int it = 0; it < 4000000; ++it) {
+    if (mbar_test_wait(bar, parity)) return true;
+    if (*abort_flag) return false;
+    __nanosleep(KU_RELAX_NS);
+  }
+  *abort_flag = 1;
+  return false;
+}
+
+// What is not an operand tile or a code slot.
+struct KuShared {
+  uint64_t q_full[2], c_full[2][kKuSingleSlots], c_empty[2][kKuSingleSlots], k_full[2], k_empty[2], v_full[2], v_empty[2], sc_full[2];
+  uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];
+  float2 sc[2][128];                     // per key of a step: scale of k, log2 of v's
+  uint32_t bad[kKuBad];                  // new rows with a v value that is not finite
+  uint32_t tmem_base;
+  int abort_flag, any_bad;
+};
+// Two row tiles: Q, Q, K, K, V, V and two slots a ring; one: Q, K, K, V, V, three slots a ring and the pipelines' (m, l).  With
+// DH = 128 the first form is all that a block can have.
 template <int DH>
 struct KuLayout {
-  static constexpr int tile = 128 * DH * 2;                       // Q, K and V tiles in fp16
+  static constexpr int tile = 128 * DH * 2;                       // an operand tile in fp16
   static constexpr int slot = 64 * DH;                            // codes of 64 keys
-  static constexpr size_t smem = 1024 + (size_t)(6 * tile + kKuPairSlots * slot > 5 * tile + kKuSingleSlots * slot
-                                                     ? 6 * tile + kKuPairSlots * slot : 5 * tile + kKuSingleSlots * slot);
+  static constexpr int pair = 6 * tile + 2 * kKuPairSlots * slot, single = 5 * tile + 2 * kKuSingleSlots * slot + 2 * 128 * 8;
+  static constexpr int body = pair > single ? pair : single;
+  static constexpr size_t smem = body + sizeof(KuShared);
+  static_assert(smem <= 232448, "a block's shared memory");
 };
 
 // Instruction descriptor: fp16 A and B, fp32 D.
@@ -80,30 +124,100 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
                "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-// Registers per thread of a warpgroup from here on (the kernel is launched with 128): softmax 152 x 256 threads,
-// converters 104 x 128, the rest 104 x 128, together the 65536 the block was launched with.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// Registers per thread of a warpgroup from here on (the kernel is launched with 96): softmax 144 x 256 threads,
+// converters 64 x 256, the rest 64 x 128, together the 61440 the block was launched with.
 template <int N>
 __device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+  return one != 0;
+}
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src),
                "r"(bytes), "r"(smem_u32(bar))
                : "memory");
 }
 
+// One bf16 row, divided by a power of two near its largest finite element, as row `row` of an fp16 operand tile.  Through
+// the row's own place in shared memory, in loops: code that runs once per CTA has to be short, because instructions that
+// are not in the cache cost far more than their work (unrolled, this and the epilogue took 30000 cycles of a 100000-cycle
+// CTA).  `odd`: values that are not finite become zero, and whether there were any is returned.
+template <int DH>
+__device__ __forceinline__ bool ku_row_to_operand(const bf16* src, bool on, uint8_t* tile, int row, bool odd, float& inv, int& ex) {
+  const uint32_t base = smem_u32(tile) + row * 128;
+  const int bytes = on ? 16 : 0;         // 0: zeros, nothing is read
+#pragma unroll 4
+  for (int c = 0; c < DH / 8; ++c)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(base + (c >> 3) * 16384 + (((c & 7) ^ (row & 7)) << 4)), "l"(src + c * 8),
+                 "r"(bytes) : "memory");
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  uint8_t* place = tile + row * 128;
+  // the largest |x| bits of both halves of all words, one three-way 16-bit maximum per two words
+  uint32_t top = 0;
+#pragma unroll 4
+  for (int c = 0; c < DH / 8; ++c) {
+    const uint4 w = *reinterpret_cast<const uint4*>(place + (c >> 3) * 16384 + (((c & 7) ^ (row & 7)) << 4));
+    top = __vimax3_u16x2(top, w.x & 0x7fff7fffu, w.y & 0x7fff7fffu);
+    top = __vimax3_u16x2(top, w.z & 0x7fff7fffu, w.w & 0x7fff7fffu);
+  }
+  uint32_t big = max(top & 0xffffu, top >> 16);
+  bool any = false;
+  if (big >= 0x7f80u) {                  // something is not finite: the largest of the rest, element by element
+    big = 0;
+#pragma unroll 1
+    for (int c = 0; c < DH / 8; ++c) {
+      uint4* v = reinterpret_cast<uint4*>(place + (c >> 3) * 16384 + (((c & 7) ^ (row & 7)) << 4));
+      uint4 w = *v;
+      big = kv8_max_finite(big, w);
+      if (odd) { any |= kv8_zero_non_finite(w); *v = w; }
+    }
+  }
+  ex = kv8_row_exp(big);
+  inv = kv8_pow2(-ex);
+#pragma unroll 2
+  for (int c = 0; c < DH / 8; ++c) {
+    uint4* v = reinterpret_cast<uint4*>(place + (c >> 3) * 16384 + (((c & 7) ^ (row & 7)) << 4));
+    uint32_t f[4];
+    kv8_bf16x8_to_half(*v, inv, f);
+    *v = make_uint4(f[0], f[1], f[2], f[3]);
+  }
+  return any;
+}
+
+// The exponent that ku_row_to_operand takes for a row.
+template <int DH>
+__device__ __forceinline__ int ku_row_exp(const bf16* src, bool on) {
+  uint32_t big = 0;
+  if (on)
+#pragma unroll 4
+    for (int c = 0; c < DH / 8; ++c) big = kv8_max_finite(big, *reinterpret_cast<const uint4*>(src + c * 8));
+  return kv8_row_exp(big);
+}
+
+__device__ __forceinline__ void bulk_prefetch(const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
+}
+
 template <int FMT, int DH>
 __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __grid_constant__ Kv8AttnArgs a, const Kv8Plan plan) {
   using Ly = KuLayout<DH>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ uint64_t q_full[2], c_full[kKuSingleSlots], c_empty[kKuSingleSlots], k_full[2], k_empty[2], v_full[2], v_empty[2];
-  __shared__ uint64_t sc_full[2], s_full[2][2], p_full[2][2], pv_done[2][2];
-  __shared__ __align__(16) float4 s_sc[2][128];        // per key of a step: scale of k, log2 and reciprocal of v's
-  __shared__ float2 s_ml[2][128];
-  __shared__ uint32_t s_bad[kKuBad];                   // new rows with a v value that is not finite
-  __shared__ uint32_t tmem_base;
-  __shared__ int abort_flag, any_bad;
+  extern __shared__ __align__(1024) uint8_t sm[];
+  KuShared& sh = *reinterpret_cast<KuShared*>(sm + Ly::body);
+  auto &q_full = sh.q_full, &k_full = sh.k_full, &k_empty = sh.k_empty, &v_full = sh.v_full, &v_empty = sh.v_empty, &sc_full = sh.sc_full;
+  auto &c_full = sh.c_full, &c_empty = sh.c_empty;
+  auto &s_full = sh.s_full, &p_full = sh.p_full, &pv_done = sh.pv_done;
+  auto& s_sc = sh.sc;
+  auto& s_bad = sh.bad;
+  int& abort_flag = sh.abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = blockIdx.x, b = blockIdx.y;
   const Kv8Seq s = kv8_seq(a, b, tid == 0 && h == 0 && blockIdx.z == 0);
@@ -129,9 +243,10 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
   uint8_t* sK = sQ + (pair ? 2 : 1) * Ly::tile;
   uint8_t* sV = sK + 2 * Ly::tile;
   uint8_t* sC = sV + 2 * Ly::tile;
+  float2(*s_ml)[128] = reinterpret_cast<float2(*)[128]>(sC + 2 * n_slots * Ly::slot);      // (one row tile)
 
   if (tid == 0) {
-    for (int i = 0; i < kKuSingleSlots; ++i) { mbar_init(&c_full[i], 1); mbar_init(&c_empty[i], 4); }
+    for (int i = 0; i < 2 * kKuSingleSlots; ++i) { mbar_init(&c_full[0][0] + i, 1); mbar_init(&c_empty[0][0] + i, 4); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&q_full[i], 4);
       mbar_init(&k_full[i], 4); mbar_init(&k_empty[i], pair ? 2 : 1);      // one release per pipeline that reads the buffer
@@ -140,418 +255,475 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       for (int hf = 0; hf < 2; ++hf) { mbar_init(&s_full[i][hf], 1); mbar_init(&p_full[i][hf], 4); mbar_init(&pv_done[i][hf], 1); }
     }
     abort_flag = 0;
-    any_bad = 0;
+    sh.any_bad = 0;
     fence_barrier_init();
   }
   if (tid < kKuBad) s_bad[tid] = 0u;
-  if (warp == 2) tmem_alloc(&tmem_base, 512);
+  if (warp == 2) tmem_alloc(&sh.tmem_base, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_base;      // pipeline p: columns 256 p + {0, 64}: S of a step's halves, each under its P; 256 p + 128: O
+  const uint32_t tmem = sh.tmem_base;      // pipeline p: columns 256 p + {0, 64}: S of a step's halves, each under its P; 256 p + 128: O
 
   // pipeline p's i-th step: every step with two row tiles, every other one with a single tile
   auto step_of = [&](int p, int i) { return pair ? i : 2 * i + p; };
   auto steps_of = [&](int p) { return pair ? n : (n + 1 - p) >> 1; };
 
   if (warp < 4) {
-   reg_dec<104>();
-   if (warp == 0) {
-    // ---- producer: 64-key slots in the order K low, K high, V low, V high of every cached step
-    const int pages = 64 >> a.c.pt_log2 > 0 ? 64 >> a.c.pt_log2 : 1, toks = 64 / pages;     // copies per slot, tokens each
-    const int total = 4 * n_cached;
-    auto page_at = [&](int t) -> int {       // this lane's page of slot t, -1: none
-      const int key = ((j0 + (t >> 2)) << 7) + ((t & 1) << 6) + lane * toks;
-      return t < total && lane < pages && key < s.len ? kv8_page(a, s.slot, key >> a.c.pt_log2) : -1;
+   reg_dec<64>();
+   if (warp == 0 || warp == 2) {
+    // ---- producers of K and of V: 64 keys a slot, two slots a cached step, a ring each.  A slot's few instructions (a wait,
+    // the byte count, a copy per page) take close to a thousand cycles beside the busy softmax warps, so each tensor
+    // has a warp of its own, and page ids are read 32 at a time, the next 32 on their way.
+    const int is_v = __shfl_sync(0xffffffffu, warp >> 1, 0);
+    const int pages = a.c.pt_log2 < 6 ? 64 >> a.c.pt_log2 : 1, bytes = (64 / pages) * DH;      // copies per slot, bytes each
+    const int total = 2 * n_cached, col0 = (int)(((long long)j0 << 7) >> a.c.pt_log2), n_cols = (s.len + a.c.pt - 1) >> a.c.pt_log2;
+    const size_t page_bytes = (size_t)a.c.hkv * a.c.pt * DH;
+    const uint8_t* base = (is_v ? a.c.v : a.c.k) + (size_t)h * a.c.pt * DH;
+    uint8_t* ring = sC + is_v * n_slots * Ly::slot;
+    uint64_t *const full = c_full[is_v], *const empty = c_empty[is_v];
+    auto ids_at = [&](int w) {            // page ids of columns col0 + 32 w + lane
+      const int col = col0 + 32 * w + lane;
+      return col < n_cols ? kv8_page(a, s.slot, col) : 0;
     };
-    int page = page_at(0), issued = 0, st = 0, use = 0;
-    for (int t = 0; t < total; ++t) {
-      const int page_next = page_at(t + 1);
-      if (use > 0 && !ta_wait(&c_empty[st], (use - 1) & 1, &abort_flag)) break;
-      const int active = __popc(__ballot_sync(0xffffffffu, page >= 0));
-      if (lane == 0) mbar_expect_tx(&c_full[st], active * toks * DH);      // 0 bytes: the slot lies behind the end, the phase completes
-      __syncwarp();
-      if (page >= 0) {
-        const int key = ((j0 + (t >> 2)) << 7) + ((t & 1) << 6) + lane * toks;
-        const uint8_t* src = (t & 2 ? a.c.v : a.c.k) + (((size_t)page * a.c.hkv + h) * a.c.pt + (key & (a.c.pt - 1))) * DH;
-        bulk_load(sC + st * Ly::slot + lane * toks * DH, src, toks * DH, &c_full[st]);
+    int window = 0, ids = ids_at(0), ids_next = ids_at(1), st = 0, use = 0, t = 0;
+#pragma unroll 1
+    for (; t < total; ++t) {
+      const int key = t << 6;             // first key of the slot, from this CTA's first
+      const int col = key >> a.c.pt_log2, live = min(pages, (s.len - (j0 << 7) - key + a.c.pt - 1) >> a.c.pt_log2);
+      if (col >= 32 * (window + 1)) {
+        ++window;
+        ids = ids_next;
+        ids_next = ids_at(window + 1);
       }
-      issued = t + 1;
-      page = page_next;
+      const int page = __shfl_sync(0xffffffffu, ids, (col + lane) & 31);
+      if (use > 0 && !ku_wait(&empty[st], (use - 1) & 1, &abort_flag)) break;
+      if (lane == 0) mbar_expect_tx(&full[st], max(live, 0) * bytes);      // 0: the slot lies behind the end, the phase completes
+      __syncwarp();
+      // two slots are little time for the way from HBM: the lines two steps on are asked into L2
+      const int ahead = col + 4 * (a.c.pt_log2 < 6 ? pages : 1);
+      const int page4 = __shfl_sync(0xffffffffu, ahead < 32 * (window + 1) ? ids : ids_next, (ahead + lane) & 31);
+      if (pair && lane < pages && t + 4 < total) bulk_prefetch(base + page4 * page_bytes + (((t + 4) << 6) & (a.c.pt - 1)) * DH, bytes);
+      if (lane < live) bulk_load(ring + st * Ly::slot + lane * bytes, base + page * page_bytes + (key & (a.c.pt - 1)) * DH, bytes, &full[st]);
       if (++st == n_slots) { st = 0; ++use; }
     }
     if (abort_flag)                  // leave no copy in flight behind
-      for (int t = max(0, issued - n_slots); t < issued; ++t)
-        for (int it = 0; it < 1000000 && !mbar_test_wait(&c_full[t % n_slots], (t / n_slots) & 1); ++it) {}
-   } else if (warp == 2) {
-    // ---- the keys' scales: one set per key, four keys (of one page) per lane; a step ahead of their use
-    auto scales = [&](int j) {
-      const int key = ((j0 + j) << 7) + lane * 4;
-      float2 sc = make_float2(0.f, 1.f);
-      if (j < n_cached && key < s.len) {
-        const size_t ph = (size_t)kv8_page(a, s.slot, key >> a.c.pt_log2) * a.c.hkv + h;
-        sc = make_float2(a.c.ks[ph], a.c.vs[ph]);
-      }
-      return sc;
-    };
-    float2 sc = scales(0);
-    for (int j = 0; j < n_cached; ++j) {
-      const int buf = j & 1, use = j >> 1;
-      const float2 next = scales(j + 1);
-      const float sv = fmaxf(sc.y, kv8_pow2(-100));
-      const float4 v = make_float4(sc.x, __log2f(sv), 1.f / sv, 0.f);
-      if (use > 0 && !ta_wait(&v_empty[buf], (use - 1) & 1, &abort_flag)) break;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) s_sc[buf][lane * 4 + q] = v;
-      __syncwarp();
-      if (lane < 4) mbar_arrive(&sc_full[buf]);      // (new rows: one arrival per converter warp)
-      sc = next;
-    }
-   } else if (lane == 0) {
-    // ---- MMA issuer of pipeline p
-    const int p = warp >> 1, np = steps_of(p), nh = 2 * np;       // half steps of 64 keys
+#pragma unroll 1
+      for (int u = max(0, t - n_slots); u < t; ++u)
+#pragma unroll 1
+        for (int it = 0; it < 1000000 && !mbar_test_wait(&full[u % n_slots], (u / n_slots) & 1); ++it) {}
+   } else {
+    // ---- MMA issuer of pipeline p.  The whole warp runs the loop and one elected lane issues, so descriptors and control
+    // flow stay in uniform registers.
+    const int p = __shfl_sync(0xffffffffu, warp >> 1, 0);
+    const int nh = 2 * steps_of(p);       // half steps of 64 keys
     constexpr uint32_t idesc_s = idesc_f16(128, 64), idesc_o = idesc_f16(128, DH) | kIdescBMnMajor;
-    const uint32_t qa = smem_u32(sQ + (pair ? p : 0) * Ly::tile);
+    const uint64_t dq = desc_sw128(smem_u32(sQ + (pair ? p : 0) * Ly::tile));
+    const uint64_t dk = desc_sw128(smem_u32(sK)), dv = desc_sw128_mn(smem_u32(sV), 16384);
     const uint32_t tS = tmem + p * 256, tO = tS + 128;
-    bool ok = np > 0 && ta_wait(&q_full[pair ? p : 0], 0, &abort_flag);
-    auto issue_s = [&](int x) -> bool {      // scores of half step x
-      const int j = step_of(p, x >> 1), buf = j & 1, hf = x & 1;
-      if (!ta_wait(&k_full[buf], (j >> 1) & 1, &abort_flag)) return false;
-      if (x >= 2 && !ta_wait(&pv_done[p][hf], ((x >> 1) - 1) & 1, &abort_flag)) return false;     // P of half x - 2 lies where S goes
-      tc_fence_after();
-      const uint32_t ka = smem_u32(sK + buf * Ly::tile) + hf * 8192;
+    bool ok = nh == 0 || ku_wait(&q_full[pair ? p : 0], 0, &abort_flag);
+    // Two things to issue, in whichever order they come ready: S of half step y, once its K is there and P of half y - 2,
+    // which lies where it goes, has been used; O += P V of half x, once P is there.  (Waiting for one before the other
+    // cost a thousand cycles a half step.)
+    int x = 0, y = 0;
+#pragma unroll 1
+    for (int it = 0; x < nh && ok; ++it) {
+      if (y < nh && y <= x + 1) {
+        const int j = step_of(p, y >> 1), buf = j & 1, hf = y & 1;
+        const bool k_ready = mbar_test_wait(&k_full[buf], (j >> 1) & 1), free = y < 2 || mbar_test_wait(&pv_done[p][hf], ((y >> 1) - 1) & 1);
+        if (__all_sync(0xffffffffu, k_ready && free)) {
+          tc_fence_after();
+          const uint64_t dk1 = dk + (uint32_t)(buf * (Ly::tile >> 4) + hf * (8192 >> 4));
+          if (elect_one()) {
 #pragma unroll
-      for (int k = 0; k < DH / 16; ++k) {
-        const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
-        mma_f16(tS + 64 * hf, desc_sw128(qa + off), desc_sw128(ka + off), idesc_s, k > 0 ? 1u : 0u);
+            for (int k = 0; k < DH / 16; ++k) {
+              const uint32_t off = ((k >> 2) * 16384 + (k & 3) * 32) >> 4;
+              mma_f16(tS + 64 * hf, dq + off, dk1 + off, idesc_s, k > 0 ? 1u : 0u);
+            }
+            mma_commit(&s_full[p][hf]);
+            if (hf == 1) mma_commit(&k_empty[buf]);
+          }
+          __syncwarp();
+          ++y;
+          it = 0;
+        }
       }
-      mma_commit(&s_full[p][hf]);
-      if (hf == 1) mma_commit(&k_empty[buf]);
-      return true;
-    };
-    if (ok) ok = issue_s(0) && issue_s(1);
-    for (int x = 0; x < nh && ok; ++x) {
-      const int j = step_of(p, x >> 1), buf = j & 1, hf = x & 1;
-      if (!ta_wait(&v_full[buf], (j >> 1) & 1, &abort_flag) || !ta_wait(&p_full[p][hf], (x >> 1) & 1, &abort_flag)) break;
-      tc_fence_after();
-      const uint64_t dv = desc_sw128_mn(smem_u32(sV + buf * Ly::tile), 16384);
+      if (x < y) {
+        const int j = step_of(p, x >> 1), buf = j & 1, hf = x & 1;
+        const bool p_ready = mbar_test_wait(&p_full[p][hf], (x >> 1) & 1), v_ready = mbar_test_wait(&v_full[buf], (j >> 1) & 1);
+        if (__all_sync(0xffffffffu, p_ready && v_ready)) {
+          tc_fence_after();
+          const uint64_t dv1 = dv + (uint32_t)(buf * (Ly::tile >> 4) + hf * 512);
+          if (elect_one()) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) mma_f16_ts(tO, tS + hf * 64 + k * 8, dv + 128 * (hf * 4 + k), idesc_o, (x > 0 || k > 0) ? 1u : 0u);
-      mma_commit(&pv_done[p][hf]);
-      if (hf == 1) mma_commit(&v_empty[buf]);
-      if (x + 2 < nh) ok = issue_s(x + 2);      // while the softmax works on half x + 1
+            for (int k = 0; k < 4; ++k) mma_f16_ts(tO, tS + hf * 64 + k * 8, dv1 + 128 * k, idesc_o, (x > 0 || k > 0) ? 1u : 0u);
+            mma_commit(&pv_done[p][hf]);
+            if (hf == 1) mma_commit(&v_empty[buf]);
+          }
+          __syncwarp();
+          ++x;
+          it = 0;
+        }
+      }
+      if (it > 0) {
+        if (__any_sync(0xffffffffu, *(volatile int*)&abort_flag != 0)) break;
+        if (it > 4000000) { abort_flag = 1; break; }
+        __nanosleep(KU_ISSUE_NS);
+      }
     }
    }
   } else if (warp >= 12) {
-    reg_dec<104>();
-    // ---- converters: codes (or new rows) to fp16 operand tiles, and the keys' scales
-    const int ct = tid - 384, cw = warp - 12;
+    reg_dec<64>();
+    // ---- converters: codes (or new rows) to fp16 operand tiles
+    // (the first four warps K, the others V and the scales: a key per thread, page id two steps and scales one step ahead)
+    const int is_v = (warp - 12) >> 2, ct = (tid - 384) & 127, cw = warp & 3;
     int st = 0, round = 0;           // next code slot and how often the ring has gone round
-    // the next slot's 64 keys -> rows row0 .. row0 + 63 of an operand tile; rows from `valid` on become zero
-    auto convert = [&](uint8_t* tile, int row0, int valid) -> bool {
-      if (!ta_wait(&c_full[st], round & 1, &abort_flag)) return false;
-      // 16 codes = two operand chunks per thread and access.  The second 64 columns of a row lie 16 KB further on, in
-      // the same banks: there the two chunks are stored in the other order, and a quarter warp's stores meet eight different bank groups.
-      constexpr int kUnits = DH / 32, kLanes = DH / 16, kRowsPerIt = 128 / kLanes;      // per thread; threads per row
-      const uint8_t* src = sC + st * Ly::slot + ct * 16;
-      uint4 w[kUnits];
-#pragma unroll
-      for (int it = 0; it < kUnits; ++it) w[it] = *reinterpret_cast<const uint4*>(src + it * 2048);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&c_empty[st]);
-      if (++st == n_slots) { st = 0; ++round; }
-      const int row1 = row0 + ct / kLanes, c = 2 * (ct % kLanes);      // rows of a thread differ by 16 or 32: one swizzle
-      const bool swap = DH == 128 && c >= 8;
-      uint8_t* base = tile + (c >> 3) * 16384 + row1 * 128;
-      uint8_t* d0 = base + ((((c & 7) + (swap ? 1 : 0)) ^ (row1 & 7)) << 4);
-      uint8_t* d1 = base + ((((c & 7) + (swap ? 0 : 1)) ^ (row1 & 7)) << 4);
-#pragma unroll
-      for (int it = 0; it < kUnits; ++it) {
-        const uint32_t x0 = swap ? w[it].z : w[it].x, x1 = swap ? w[it].w : w[it].y, x2 = swap ? w[it].x : w[it].z, x3 = swap ? w[it].y : w[it].w;
-        uint4 f, g;
-        kv8_unpack4<FMT>(x0, f.x, f.y);
-        kv8_unpack4<FMT>(x1, f.z, f.w);
-        kv8_unpack4<FMT>(x2, g.x, g.y);
-        kv8_unpack4<FMT>(x3, g.z, g.w);
-        if (valid < 128 && row1 + it * kRowsPerIt >= valid) f = g = make_uint4(0u, 0u, 0u, 0u);
-        *reinterpret_cast<uint4*>(d0 + it * kRowsPerIt * 128) = f;
-        *reinterpret_cast<uint4*>(d1 + it * kRowsPerIt * 128) = g;
-      }
-      return true;
-    };
+    const uint8_t* const ring = sC + is_v * n_slots * Ly::slot;
+    uint8_t* const tiles = is_v ? sV : sK;
+    uint64_t *const full = is_v ? v_full : k_full, *const empty = is_v ? v_empty : k_empty;
+    // 16 codes = two operand chunks per thread and access.  The second 64 columns of a row lie 16 KB further on, in the same
+    // banks: there the two chunks are stored in the other order, and a quarter warp's stores meet eight different bank
+    // groups.  A thread's rows are 16 or 32 apart: one swizzle for all of them.
+    constexpr int kUnits = DH / 32, kLanes = DH / 16, kRowsPerIt = 128 / kLanes;      // per thread; threads per row
+    const int row_in = ct / kLanes, c = 2 * (ct % kLanes);
+    const bool swap = DH == 128 && c >= 8;
+    const uint32_t d0 = (c >> 3) * 16384 + row_in * 128 + ((((c & 7) + (swap ? 1 : 0)) ^ (row_in & 7)) << 4);
+    const uint32_t d1 = (c >> 3) * 16384 + row_in * 128 + ((((c & 7) + (swap ? 0 : 1)) ^ (row_in & 7)) << 4);
     auto publish = [&](uint64_t* bar) {
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
-    for (int j = 0; j < n; ++j) {
-      const int buf = j & 1, use = j >> 1;
-      uint8_t *tk = sK + buf * Ly::tile, *tv = sV + buf * Ly::tile;
-      if (use > 0 && !ta_wait(&k_empty[buf], (use - 1) & 1, &abort_flag)) break;
-      if (j < n_cached) {
-        const int valid = min(128, s.len - ((j0 + j) << 7));
-        bool ok = true;
+    auto page_of = [&](int j) -> int {       // page of this thread's key of step j (the producers report bad ids)
+      const int key = ((j0 + j) << 7) + ct;
+      if (j >= n_cached || key >= s.len) return -1;
+      const int p = a.table[(size_t)s.slot * a.max_pages + (key >> a.c.pt_log2)];
+      return (unsigned)p < (unsigned)a.c.n_pages ? p : 0;
+    };
+    auto scales_of = [&](int page) {
+      const size_t ph = (size_t)page * a.c.hkv + h;
+      return page < 0 ? make_float2(0.f, 1.f) : make_float2(a.c.ks[ph], a.c.vs[ph]);
+    };
+    float2 sc = is_v ? scales_of(page_of(0)) : make_float2(0.f, 1.f);
+    int page_next = is_v ? page_of(1) : -1;
+    bool ok = true;
 #pragma unroll 1
-        for (int q = 0; q < 4 && ok; ++q) {        // K low, K high, V low, V high
-          if (q == 2 && use > 0 && !ta_wait(&v_empty[buf], (use - 1) & 1, &abort_flag)) { ok = false; break; }
-          ok = convert(q < 2 ? tk : tv, (q & 1) * 64, valid);
-          if (ok && (q & 1)) publish(q == 1 ? &k_full[buf] : &v_full[buf]);
+    for (int j = 0; j < n && ok; ++j) {
+      const int buf = j & 1, use = j >> 1;
+      if (use > 0) ok = ku_wait_relaxed(&empty[buf], (use - 1) & 1, &abort_flag);
+      if (!ok) break;
+      if (j < n_cached) {
+        if (is_v) {
+          const float sv = fmaxf(sc.y, kv8_pow2(-100));
+          s_sc[buf][ct] = make_float2(sc.x, __log2f(sv));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sc_full[buf]);
+          sc = scales_of(page_next);
+          page_next = page_of(j + 2);
+        }
+        const int valid = s.len - ((j0 + j) << 7);        // rows from here on become zero
+#pragma unroll 1
+        for (int q = 0; q < 2; ++q) {        // 64 keys each
+          uint8_t* tile = tiles + buf * Ly::tile + q * 8192;
+          ok = ku_wait_relaxed(&c_full[is_v][st], round & 1, &abort_flag);
+          if (!ok) break;
+          const uint8_t* src = ring + st * Ly::slot + ct * 16;
+          uint4 w[kUnits];
+#pragma unroll
+          for (int it = 0; it < kUnits; ++it) w[it] = *reinterpret_cast<const uint4*>(src + it * 2048);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&c_empty[is_v][st]);
+          if (++st == n_slots) { st = 0; ++round; }
+#pragma unroll
+          for (int it = 0; it < kUnits; ++it) {
+            const bool live = q * 64 + row_in + it * kRowsPerIt < valid;
+            const uint32_t x0 = swap ? w[it].z : w[it].x, x1 = swap ? w[it].w : w[it].y, x2 = swap ? w[it].x : w[it].z, x3 = swap ? w[it].y : w[it].w;
+            uint4 f, g;
+            kv8_unpack4<FMT>(live ? x0 : 0u, f.x, f.y);      // code 0 is zero in both formats
+            kv8_unpack4<FMT>(live ? x1 : 0u, f.z, f.w);
+            kv8_unpack4<FMT>(live ? x2 : 0u, g.x, g.y);
+            kv8_unpack4<FMT>(live ? x3 : 0u, g.z, g.w);
+            *reinterpret_cast<uint4*>(tile + d0 + it * kRowsPerIt * 128) = f;
+            *reinterpret_cast<uint4*>(tile + d1 + it * kRowsPerIt * 128) = g;
+          }
         }
         if (!ok) break;
+        publish(&full[buf]);
       } else {
-        const int y0 = (j0 + j - tl.cached) << 7, y = y0 + ct;          // new row of this thread
+        // 128 new rows, one per thread, each divided by a power of two of its own
+        const int y0 = (j0 + j - tl.cached) << 7, y = y0 + ct;
         const bool on = y < s.rows;
-        const size_t off = (size_t)((long long)b * a.rows + (on ? y : 0)) * a.new_stride + (size_t)h * DH;
-        int ek = -64, ev = -64;
-#pragma unroll
-        for (int is_v = 0; is_v < 2; ++is_v) {
-          const uint4* src = reinterpret_cast<const uint4*>((is_v ? a.v_new : a.k_new) + off);
-          uint8_t* tile = is_v ? tv : tk;
-          uint32_t big = 0;
-          bool odd = false;
-#pragma unroll 4
-          for (int c = 0; c < DH / 8; ++c) {
-            uint4 v = on ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-            if (is_v) odd |= kv8_zero_non_finite(v);
-            big = kv8_max_finite(big, v);
-          }
-          const int ex = kv8_row_exp(big);
-          const float inv = kv8_pow2(-ex);
-          if (is_v) ev = ex; else ek = ex;
-          if (is_v && use > 0 && !ta_wait(&v_empty[buf], (use - 1) & 1, &abort_flag)) break;
-#pragma unroll 4
-          for (int c = 0; c < DH / 8; ++c) {      // the row once more, from the cache, instead of 64 registers
-            uint4 v = on ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-            if (is_v) kv8_zero_non_finite(v);
-            uint32_t f[4];
-            kv8_bf16x8_to_half(v, inv, f);
-            *reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + ct * 128 + (((c & 7) ^ (ct & 7)) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
-          }
-          if (is_v) {
-            const uint32_t bits = __ballot_sync(0xffffffffu, odd);
-            if (lane == 0 && bits != 0u) { s_bad[(y0 >> 5) + cw] = bits; any_bad = 1; }
-            s_sc[buf][ct] = make_float4(kv8_pow2(ek), (float)ev, inv, 0.f);
-          }
-          publish(is_v ? &v_full[buf] : &k_full[buf]);
+        const bf16* src = (is_v ? a.v_new : a.k_new) + (size_t)((long long)b * a.rows + (on ? y : 0)) * a.new_stride + (size_t)h * DH;
+        float inv;
+        int ex;
+        const bool odd = ku_row_to_operand<DH>(src, on, tiles + buf * Ly::tile, ct, is_v != 0, inv, ex);
+        if (is_v) {
+          const uint32_t bits = __ballot_sync(0xffffffffu, odd);
+          if (lane == 0 && bits != 0u) { s_bad[(y0 >> 5) + cw] = bits; sh.any_bad = 1; }
+          // the key's scale is its row's power of two as well: the V group takes it from the row itself
+          s_sc[buf][ct] = make_float2(kv8_pow2(ku_row_exp<DH>(a.k_new + (src - a.v_new), on)), (float)ex);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sc_full[buf]);
         }
-        if (abort_flag) break;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sc_full[buf]);
+        publish(&full[buf]);
       }
     }
   } else {
-    reg_inc<152>();
+    reg_inc<144>();
     // ---- softmax of pipeline p: thread = row of its tile = tensor-memory lane
     const int p = (warp - 4) >> 2, wq = warp & 3, row = wq * 32 + lane, np = steps_of(p);
-    const int i_row = (tl.first + (pair ? p : 0)) * 128 + row;
+    const int tile = tl.first + (pair ? p : 0), i_row = tile * 128 + row;
     const bool on = i_row < Nv;
-    const int r = on ? i_row / a.G : 0;
+    const int r = i_row / a.G, g_head = h * a.G + i_row - r * a.G;       // (of rows that exist)
     const uint32_t tS = tmem + ((uint32_t)(wq * 32) << 16) + p * 256, tO = tS + 128;
-    float crow;
-    {
-      const uint4* qp = reinterpret_cast<const uint4*>(a.q + (size_t)((long long)b * a.rows + r) * a.q_stride +
-                                                       (size_t)(h * a.G + (on ? i_row % a.G : 0)) * DH);
-      uint32_t big = 0;
-#pragma unroll
-      for (int c = 0; c < DH / 8; ++c) big = kv8_max_finite(big, on ? qp[c] : make_uint4(0u, 0u, 0u, 0u));
-      const int ex = kv8_row_exp(big);
+    float crow = 0.f;
+    if (pair || p == 0) {
+      float inv;
+      int ex;
+      ku_row_to_operand<DH>(a.q + (on ? (size_t)((long long)b * a.rows + r) * a.q_stride + (size_t)g_head * DH : 0), on,
+                            sQ + (pair ? p : 0) * Ly::tile, row, false, inv, ex);
       crow = a.scale_log2e * kv8_pow2(ex);
-      if (pair || p == 0) {
-        const float inv = kv8_pow2(-ex);
-        uint8_t* tile = sQ + (pair ? p : 0) * Ly::tile;
-#pragma unroll
-        for (int c = 0; c < DH / 8; ++c) {
-          uint32_t f[4];
-          kv8_bf16x8_to_half(on ? qp[c] : make_uint4(0u, 0u, 0u, 0u), inv, f);
-          *reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
-        }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&q_full[pair ? p : 0]);
+      if (!pair) s_ml[0][row].x = crow;
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_full[pair ? p : 0]);
+    }
+    unsigned long long among = 0;         // a tree: the new rows that this row sees, as bits
+    if (a.mask != nullptr) {
+      const uint8_t* m = a.mask + (size_t)b * a.rows * a.rows;
+      const int r_lo = __shfl_sync(0xffffffffu, r, 0), r_hi = min(s.rows - 1, __shfl_sync(0xffffffffu, r, 31));     // the warp's rows
+#pragma unroll 4
+      for (int x = r_lo; x <= r_hi; ++x) {
+        const uint32_t lo = __ballot_sync(0xffffffffu, lane < s.rows && m[x * a.rows + lane] != 0);
+        const uint32_t hi = __ballot_sync(0xffffffffu, lane + 32 < s.rows && m[x * a.rows + lane + 32] != 0);
+        if (x == r) among = (unsigned long long)hi << 32 | lo;
       }
     }
-    unsigned long long among = 0;          // tree: the new rows that this row sees
-    if (a.mask != nullptr && on)
-      for (int y = 0; y < s.rows; ++y)
-        if (kv8_sees(a, b, r, y)) among |= 1ull << y;
+    if (!pair) {                          // both pipelines of a single tile have the same rows
+      asm volatile("bar.sync 1, 256;" ::: "memory");       // the softmax warps
+      crow = s_ml[0][row].x;
+      asm volatile("bar.sync 1, 256;" ::: "memory");       // s_ml is used again below
+    }
     float m_ref = -INFINITY, l = 0.f;
     bool ok = true;
-    for (int i = 0; i < np && ok; ++i) {
-      const int j = step_of(p, i), buf = j & 1;
-      if (!ta_wait(&sc_full[buf], (j >> 1) & 1, &abort_flag)) { ok = false; break; }      // the keys' scales
+    for (int x = 0; x < 2 * np; ++x) {        // half steps of 64 keys
+      const int i = x >> 1, hf = x & 1, j = step_of(p, i), buf = j & 1;
+      ok = (hf == 1 || ku_wait(&sc_full[buf], (j >> 1) & 1, &abort_flag)) && ku_wait(&s_full[p][hf], i & 1, &abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      const float2* scp = &s_sc[buf][hf * 64];
       const bool cached = j < n_cached;
       const int left = s.len - ((j0 + j) << 7);                              // cached keys from this step on
+      // a new reference maximum rescales what O holds, once the half step before has been added to it
+      auto raise = [&](float mt) -> bool {
+        float alpha = 1.f;
+        if (mt > m_ref + 8.f) {             // also the first visible key (m_ref = -inf)
+          alpha = m_ref == -INFINITY ? 1.f : kv8_ex2(m_ref - mt);
+          m_ref = mt;
+          l *= alpha;
+        }
+        if (x > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+          if (!ku_wait(&pv_done[p][hf ^ 1], (hf ? i : i - 1) & 1, &abort_flag)) return false;
+          tc_fence_after();
 #pragma unroll 1
-      for (int hf = 0; hf < 2; ++hf) {
-        if (!ta_wait(&s_full[p][hf], i & 1, &abort_flag)) { ok = false; break; }
-        tc_fence_after();
-        const float4* scp = &s_sc[buf][hf * 64];
-        // a new reference rescales what O holds, once the half step before has been added to it
-        auto raise = [&](float mt) -> bool {
-          float alpha = 1.f;
-          if (mt > m_ref + 8.f) {           // also the first visible key (m_ref = -inf)
-            alpha = m_ref == -INFINITY ? 1.f : kv8_ex2(m_ref - mt);
-            m_ref = mt;
-            l *= alpha;
-          }
-          if ((i > 0 || hf > 0) && __any_sync(0xffffffffu, alpha != 1.f)) {
-            if (!ta_wait(&pv_done[p][hf ^ 1], (hf ? i : i - 1) & 1, &abort_flag)) return false;
-            tc_fence_after();
-#pragma unroll 1
-            for (int cb = 0; cb < DH; cb += 16) {
-              uint32_t rr[16];
-              tmem_ld16(tO + cb, rr);
-              tmem_ld_wait();
-#pragma unroll
-              for (int q = 0; q < 16; ++q) rr[q] = __float_as_uint(__uint_as_float(rr[q]) * alpha);
-              tmem_st16(tO + cb, rr);
-            }
-            tmem_st_wait();
-          }
-          return true;
-        };
-        if (cached && left >= 128) {
-          // 64 cached keys: one set of scales per 16
-          float sv[64], mul[4], add[4], mt = -INFINITY;
-          tmem_ld64(tS + hf * 64, sv);
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const float4 c = scp[g * 16];
-            mul[g] = crow * c.x; add[g] = c.y;
-            float x0 = fmaxf(sv[16 * g], sv[16 * g + 1]), x1 = fmaxf(sv[16 * g + 2], sv[16 * g + 3]);
-#pragma unroll
-            for (int q = 4; q < 16; q += 4) {
-              x0 = fmaxf(x0, fmaxf(sv[16 * g + q], sv[16 * g + q + 1]));
-              x1 = fmaxf(x1, fmaxf(sv[16 * g + q + 2], sv[16 * g + q + 3]));
-            }
-            mt = fmaxf(mt, fmaf(fmaxf(x0, x1), mul[g], add[g]));
-          }
-          ok = raise(mt);
-          if (!ok) break;
-          const float mu = m_ref == -INFINITY ? 0.f : m_ref;
-          uint32_t pk[32];
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const float sub = add[g] - mu;
-            const f32x2 mul2 = pack2(mul[g], mul[g]), sub2 = pack2(sub, sub);
-            f32x2 ls = pack2(0.f, 0.f);
-#pragma unroll
-            for (int q = 0; q < 16; q += 2) {
-              float x0, x1;
-              unpack2(fma2(pack2(sv[16 * g + q], sv[16 * g + q + 1]), mul2, sub2), x0, x1);
-              const float p0 = kv8_ex2(x0), p1 = kv8_ex2(x1);
-              ls = add2(ls, pack2(p0, p1));
-              const __half2 v2 = __floats2half2_rn(p0, p1);
-              pk[8 * g + q / 2] = *reinterpret_cast<const uint32_t*>(&v2);
-            }
-            float l0, l1;
-            unpack2(ls, l0, l1);
-            l = fmaf(l0 + l1, scp[g * 16].z, l);
-          }
-          tmem_st32(tS + hf * 64, pk);      // over the scores it came from
-        } else {
-          // the end of the cache, or new rows with a scale per key: 16 columns at a time, twice, in little code
-          int hi;                           // last visible column, if they are a prefix
-          if (cached) hi = left - 1 - hf * 64;
-          else hi = min(r, s.rows - 1) - ((j0 + j - tl.cached) << 7) - hf * 64;
-          unsigned long long vis = hi < 0 ? 0ull : hi >= 63 ? ~0ull : (2ull << hi) - 1ull;
-          if (!cached && a.mask != nullptr) vis = hf == 0 && j0 + j == tl.cached ? among : 0ull;
-          if (!on) vis = 0ull;
-          auto scores = [&](int c16, float (&x)[16]) {
+          for (int cb = 0; cb < DH; cb += 16) {
             uint32_t rr[16];
-            tmem_ld16(tS + hf * 64 + c16, rr);
+            tmem_ld16(tO + cb, rr);
             tmem_ld_wait();
-            const uint32_t v = (uint32_t)(vis >> c16);
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-              const float4 c = scp[c16 + q];
-              const float y = fmaf(__uint_as_float(rr[q]), crow * c.x, c.y);
-              x[q] = (v >> q) & 1u ? y : -INFINITY;
-            }
-          };
-          float x[16], mt = -INFINITY;
-#pragma unroll 1
-          for (int c16 = 0; c16 < 64; c16 += 16) {
-            scores(c16, x);
-#pragma unroll
-            for (int q = 0; q < 16; ++q) mt = fmaxf(mt, x[q]);
+            for (int q = 0; q < 16; ++q) rr[q] = __float_as_uint(__uint_as_float(rr[q]) * alpha);
+            tmem_st16(tO + cb, rr);
           }
-          ok = raise(mt);
-          if (!ok) break;
-          const float mu = m_ref == -INFINITY ? 0.f : m_ref;
+          tmem_st_wait();
+        }
+        return true;
+      };
+      if (cached && left >= 128) {
+        // 64 cached keys, one set of scales per 16, against the reference so far.  No maximum first: P in fp16 holds up to
+        // 2^16, so only when the half step's weights add up to more than 2^14 (and at the very first) the maximum is taken and the
+        // half step done again.
+        bool first = x == 0;
 #pragma unroll 1
-          for (int c16 = 0; c16 < 64; c16 += 16) {
-            scores(c16, x);
-            uint32_t pk[8];
+        for (;;) {
+          if (first) {
+            float mt = -INFINITY;
+#pragma unroll 1
+            for (int g = 0; g < 4; ++g) {
+              uint32_t rr[16];
+              tmem_ld16(tS + hf * 64 + g * 16, rr);
+              tmem_ld_wait();
+              const float2 c = scp[g * 16];
+              float x0 = __uint_as_float(rr[0]);
 #pragma unroll
-            for (int q = 0; q < 16; q += 2) {
-              const float p0 = kv8_ex2(x[q] - mu), p1 = kv8_ex2(x[q + 1] - mu);
-              l = fmaf(p0, scp[c16 + q].z, l);
-              l = fmaf(p1, scp[c16 + q + 1].z, l);
-              const __half2 v2 = __floats2half2_rn(p0, p1);
-              pk[q / 2] = *reinterpret_cast<const uint32_t*>(&v2);
+              for (int q = 1; q < 15; q += 2) x0 = max3(x0, __uint_as_float(rr[q]), __uint_as_float(rr[q + 1]));
+              mt = fmaxf(mt, fmaf(fmaxf(x0, __uint_as_float(rr[15])), crow * c.x, c.y));
             }
-            tmem_st8(tS + hf * 64 + c16 / 2, pk);      // over columns read before: c16 / 2 + 7 < c16 + 16
+            ok = raise(mt);
+            if (!ok) break;
+          }
+          const float mu = m_ref == -INFINITY ? 0.f : m_ref;
+          float l_new = l;
+          uint32_t pk[32];
+          float sum = 0.f;
+          {
+            float rr[64];
+            tmem_ld64(tS + hf * 64, rr);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const float2 c = scp[g * 16];
+              const float mul = crow * c.x, sub = c.y - mu;
+              const f32x2 mul2 = pack2(mul, mul), sub2 = pack2(sub, sub);
+              f32x2 ls = pack2(0.f, 0.f);
+#pragma unroll
+              for (int q = 0; q < 16; q += 2) {
+                float x0, x1;
+                unpack2(fma2(pack2(rr[16 * g + q], rr[16 * g + q + 1]), mul2, sub2), x0, x1);
+                const float p0 = kv8_ex2(x0), p1 = kv8_ex2(x1);
+                ls = add2(ls, pack2(p0, p1));
+                const __half2 v2 = __floats2half2_rn(p0, p1);
+                pk[8 * g + q / 2] = *reinterpret_cast<const uint32_t*>(&v2);
+              }
+              float l0, l1;
+              unpack2(ls, l0, l1);
+              sum += l0 + l1;
+              l_new = fmaf(l0 + l1, kv8_ex2(-c.y), l_new);      // back to the weights alone
+            }
+          }
+          const bool fine = sum <= 16384.f;
+          if (first || !__any_sync(0xffffffffu, !fine)) {
+            l = l_new;
+            tmem_st32(tS + hf * 64, pk);    // over the scores it came from
+            break;
+          }
+          first = true;
+        }
+        if (!ok) break;
+      } else {
+        // the end of the cache, or new rows with a scale per key: 16 columns at a time, twice, in little code
+        int hi;                           // last visible column, if they are a prefix
+        if (cached) hi = left - 1 - hf * 64;
+        else hi = min(r, s.rows - 1) - ((j0 + j - tl.cached) << 7) - hf * 64;
+        unsigned long long vis = hi < 0 ? 0ull : hi >= 63 ? ~0ull : (2ull << hi) - 1ull;
+        if (!cached && a.mask != nullptr) vis = hf == 0 && j0 + j == tl.cached ? among : 0ull;
+        if (!on) vis = 0ull;
+        float mt = -INFINITY, mu = 0.f;
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {         // the maximum, then the weights
+          if (pass == 1) {
+            ok = raise(mt);
+            if (!ok) break;
+            mu = m_ref == -INFINITY ? 0.f : m_ref;
+          }
+#pragma unroll 1
+          for (int c0 = 0; c0 < 64; c0 += 16) {
+            const uint32_t v = (uint32_t)(vis >> c0) & 0xffffu;
+            uint32_t pk[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+            if (__any_sync(0xffffffffu, v != 0u)) {    // columns that no row of the warp sees have no weight
+              uint32_t rr[16];
+              tmem_ld16(tS + hf * 64 + c0, rr);
+              tmem_ld_wait();
+              float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+              for (int q = 0; q < 16; ++q) {
+                const float2 c = scp[c0 + q];
+                float y = fmaf(__uint_as_float(rr[q]), crow * c.x, c.y);
+                y = (v >> q) & 1u ? y : -INFINITY;
+                if (pass == 0) {
+                  mt = fmaxf(mt, y);
+                } else {
+                  y = kv8_ex2(y - mu);
+                  const float w = y * kv8_ex2(-c.y);
+                  if (q & 1) l1 += w; else l0 += w;
+                  rr[q] = __float_as_uint(y);
+                }
+              }
+              if (pass == 1) {
+                l += l0 + l1;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                  const __half2 v2 = __floats2half2_rn(__uint_as_float(rr[2 * q]), __uint_as_float(rr[2 * q + 1]));
+                  pk[q] = *reinterpret_cast<const uint32_t*>(&v2);
+                }
+              }
+            }
+            if (pass == 1) tmem_st8(tS + hf * 64 + c0 / 2, pk);      // over columns read before: c0 / 2 + 7 < c0 + 16
           }
         }
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[p][hf]);
+        if (!ok) break;
       }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_full[p][hf]);
     }
-    if (ok && np > 0) ok = ta_wait(&pv_done[p][1], (np - 1) & 1, &abort_flag);
-    s_ml[p][row] = make_float2(m_ref, l);
-    tc_fence_before();
-    asm volatile("bar.sync 1, 256;" ::: "memory");       // the softmax warps
+    if (ok && np > 0) ok = ku_wait(&pv_done[p][1], (np - 1) & 1, &abort_flag);
+    if (!pair) {
+      s_ml[p][row] = make_float2(m_ref, l);
+      tc_fence_before();
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+    }
     tc_fence_after();
     // ---- results: a pipeline's own tile, or the join of the two pipelines of a single tile (half of the columns each)
     if (!abort_flag) {
-      const int tile = tl.first + (pair ? p : 0);
       const uint32_t tR = tmem + ((uint32_t)(wq * 32) << 16) + 128;
       const bool two = !pair && n > 1;
-      const float2 ml0 = s_ml[pair ? p : 0][row], ml1 = two ? s_ml[1][row] : make_float2(-INFINITY, 0.f);
+      const float2 ml0 = pair ? make_float2(m_ref, l) : s_ml[0][row], ml1 = two ? s_ml[1][row] : make_float2(-INFINITY, 0.f);
       const float M = fmaxf(ml0.x, ml1.x);
-      const float f0 = ml0.y == 0.f ? 0.f : two ? exp2f(ml0.x - M) : 1.f, f1 = ml1.y == 0.f ? 0.f : exp2f(ml1.x - M);
+      float f0 = ml0.y == 0.f ? 0.f : two ? exp2f(ml0.x - M) : 1.f, f1 = ml1.y == 0.f ? 0.f : exp2f(ml1.x - M);
       const float L = ml0.y * f0 + ml1.y * f1;
+      const bool whole = tl.split.n == 1;
+      if (whole) {                        // finished rows: divided by the sum; without keys, or beyond the rows that exist, zero
+        const float inv = L == 0.f || !on ? 0.f : 1.f / L;
+        f0 = f0 == 0.f || !on ? 0.f : f0 * inv;
+        f1 = f1 == 0.f || !on ? 0.f : f1 * inv;
+      }
       const int c_lo = pair ? 0 : p * (DH / 2), c_hi = pair ? DH : c_lo + DH / 2;
       const size_t part = (((size_t)(b * a.c.hkv + h) * plan.n_tiles + tile) * plan.max_chunks + chunk_id) * 128 + row;
-      const bool bad = any_bad != 0;
+      bf16* out = a.out + ((size_t)((long long)b * a.rows + r) * a.hq + g_head) * DH;
+      const bool bad = sh.any_bad != 0 && on;
 #pragma unroll 1
-      for (int cb = c_lo; cb < c_hi; cb += 16) {
-        uint32_t r0[16], r1[16];
-        tmem_ld16(tR + (pair ? p * 256 : 0) + cb, r0);
-        if (two) tmem_ld16(tR + 256 + cb, r1);
+      for (int cb = c_lo; cb < c_hi; cb += 8) {
+        uint32_t r0[8], r1[8];
+        tmem_ld8(tR + (pair ? p * 256 : 0) + cb, r0);
+        if (two) tmem_ld8(tR + 256 + cb, r1);
         tmem_ld_wait();
-        float o[16];
+        float o[8];
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
+        for (int q = 0; q < 8; ++q) {
           o[q] = f0 == 0.f ? 0.f : __uint_as_float(r0[q]) * f0;
           if (two && f1 != 0.f) o[q] += __uint_as_float(r1[q]) * f1;
         }
-        if (i_row < N) {
-          if (bad && i_row < Nv) {            // values that are not finite reach exactly the rows that see them
-            const int r = i_row / a.G;
-            for (int y = 0; y < s.rows; ++y) {
-              if (!((s_bad[y >> 5] >> (y & 31)) & 1u) || !kv8_sees(a, b, r, y)) continue;
-              const bf16* v = a.v_new + (size_t)((long long)b * a.rows + y) * a.new_stride + (size_t)h * DH + cb;
+        if (bad) {                        // values that are not finite reach exactly the rows that see them
+#pragma unroll 1
+          for (int y = 0; y < s.rows; ++y) {
+            if (!((s_bad[y >> 5] >> (y & 31)) & 1u) || !kv8_sees(a, b, r, y)) continue;
+            const uint4 v = *reinterpret_cast<const uint4*>(a.v_new + (size_t)((long long)b * a.rows + y) * a.new_stride + (size_t)h * DH + cb);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-              for (int q = 0; q < 16; ++q) {
-                const float x = __bfloat162float(v[q]);
-                if (!isfinite(x)) o[q] += x;
-              }
+            for (int q = 0; q < 8; ++q) {
+              const float z = __uint_as_float(q & 1 ? w[q / 2] & 0xffff0000u : w[q / 2] << 16);
+              if (!isfinite(z)) o[q] += z;
             }
           }
+        }
+        if (i_row < N) {
+          if (whole) {
+            uint32_t w[4];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float4 v = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-            if (tl.split.n == 1) kv8_store_row(a, b, h, i_row, i_row < Nv, L, cb / 4 + q, v);
-            else *reinterpret_cast<float4*>(plan.o_part + part * DH + cb + 4 * q) = v;
+            for (int q = 0; q < 4; ++q) {
+              const __nv_bfloat162 v2 = __floats2bfloat162_rn(o[2 * q], o[2 * q + 1]);
+              w[q] = *reinterpret_cast<const uint32_t*>(&v2);
+            }
+            *reinterpret_cast<uint4*>(out + cb) = make_uint4(w[0], w[1], w[2], w[3]);
+          } else {
+            float4* dst = reinterpret_cast<float4*>(plan.o_part + part * DH + cb);
+            dst[0] = make_float4(o[0], o[1], o[2], o[3]);
+            dst[1] = make_float4(o[4], o[5], o[6], o[7]);
           }
         }
         __syncwarp();
       }
-      if (tl.split.n > 1 && c_lo == 0 && i_row < N) *reinterpret_cast<float2*>(plan.ml_part + part * 2) = make_float2(M, L);
+      if (!whole && c_lo == 0 && i_row < N) *reinterpret_cast<float2*>(plan.ml_part + part * 2) = make_float2(M, L);
     }
   }
   tc_fence_before();
