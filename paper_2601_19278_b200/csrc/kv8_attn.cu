@@ -22,93 +22,105 @@
 namespace dart {
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------
-// What bounds it is the stream of K and V bytes, so nothing is staged: a warp takes 16 keys at a time and every lane loads
-// exactly the bytes that its own tensor-core fragments need, 16 (or 8) at a time, one group ahead of the arithmetic.
-//   S = Q K^T   mma m16n8k16, rows x keys.  The order of the contraction index is free as long as Q and K agree: lane t of a
-//               key's quad takes d = [t * DH/4, (t+1) * DH/4), whole 16-byte words of the key's row.
+// What bounds it is the stream of K and V bytes, and that takes bytes in flight: about 60 KB per SM, which registers cannot
+// hold beside the accumulators (with one group of 16 keys ahead in registers, 48 KB per SM: 5.0 TB/s; @STREAM).  Every warp
+// therefore has a ring of its own in shared memory, kStStages groups of 16 keys deep, filled by 16-byte asynchronous
+// copies; rows are laid out so that the reads below meet no bank twice.  From there every lane reads exactly the bytes that
+// its own tensor-core fragments need:
+//   S^T = K Q^T    mma m16n8k16 with the 16 keys as M.  The order of the contraction index is free as long as Q and K agree:
+//                  lane t of a key's quad takes d = [t * DH/4, (t+1) * DH/4), whole 16-byte words of the key's row.
 //   O^T = V^T P^T  the same instruction with d as M: its A operand wants pairs of neighbouring keys, which two bytes of
-//               two keys' words give by one byte permutation before the conversion; the scores come out of the first product
-//               exactly where the second wants its B operand, so P never leaves its lane.
-// m moves only when a score exceeds it by 2^8: the common case has no shuffles at all.
-constexpr int kStWarps = 4;
+//                  two keys' words give by one byte permutation before the conversion; P^T is the first product's result
+//                  transposed in 8 x 8 blocks (movmatrix).  Both products give a lane the same two rows, so m and l are its own.
+// m moves only when a score exceeds it by 2^8: the common case has no shuffles at all.  Instructions count next to the bytes
+// (with rows as M in the first product, half of M empty, and scales and addresses from global memory a group of 4 KB took 319
+// of them and the batch of 64 tokens 120 us): scales, their logarithms and the page ids of the CTA's groups are laid out in
+// shared memory once.
+constexpr int kStWarps = 4, kStStages = 3;
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-
-// Bytes of one group of 16 keys that a lane holds: K of keys g and g + 8, V of keys 2t, 2t+1, 2t+8, 2t+9.
-template <int DH>
-struct Group {
-  uint32_t k[2][DH / 16];      // DH/4 bytes each
-  uint32_t v[4][DH / 32];      // DH/8 bytes each
-};
-template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&r)[N], const uint8_t* p) {
-  static_assert(N == 2 || N % 4 == 0, "");
-  if constexpr (N == 2) {
-    const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
-    r[0] = x.x; r[1] = x.y;
-  } else {
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-      const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + i);
-      r[4 * i] = x.x; r[4 * i + 1] = x.y; r[4 * i + 2] = x.z; r[4 * i + 3] = x.w;
-    }
-  }
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 
-// NT = 1: up to 8 rows (the second half of the first product's M is empty), 2: up to 16.
+// Place of the 16-byte chunk c of row r in a [16][DH] byte tile: lines of 128 bytes, chunks exchanged within a line so that
+// lanes (g, t) that read chunk f(t) of rows g, or chunk g of rows 2t, meet different banks.
+template <int DH>
+__device__ __forceinline__ uint32_t st_place(int r, int c) {
+  if (DH == 128) return r * 128 + ((c ^ (r & 7)) << 4);
+  const int line = r >> 1;
+  return line * 128 + (((((r & 1) << 2) | c) ^ ((line * 2) & 7)) << 4);
+}
+
+// Shared memory: the warps' rings, later their O; then the groups' scales and pages.
+template <int DH, int NT>
+constexpr __host__ __device__ int st_body() {
+  return kStWarps * kStStages * 2 * 16 * DH > kStWarps * 8 * NT * DH * 4 ? kStWarps * kStStages * 2 * 16 * DH : kStWarps * 8 * NT * DH * 4;
+}
+
+// NT tiles of 8 rows: up to 8 or up to 16 rows.
 template <int FMT, int DH, int NT>
-__global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_stream_kernel(const __grid_constant__ Kv8AttnArgs a,
+__global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 4 : 2) kv8_attn_stream_kernel(const __grid_constant__ Kv8AttnArgs a,
                                                                                         const Kv8Plan plan) {
   constexpr int MT = DH / 16, KW = DH / 16;     // d tiles of the second product; words of a lane's piece of a key
   constexpr int NR = 8 * NT;
   extern __shared__ __align__(16) unsigned char st_smem[];
-  int* s_page = reinterpret_cast<int*>(st_smem);                 // [plan.chunk / 16] page of every group of 16 keys
+  constexpr int kTile = 16 * DH;                                 // codes of 16 keys
+  unsigned char* ring = st_smem + (threadIdx.x >> 5) * (kStStages * 2 * kTile);                       // this warp's
+  float(*s_o)[NR][DH] = reinterpret_cast<float(*)[NR][DH]>(st_smem);                                  // in the end, all warps' O
+  float4* s_group = reinterpret_cast<float4*>(st_smem + st_body<DH, NT>());     // per group of 16 keys: k's scale, log2 and reciprocal of v's, page id
   __shared__ float s_m[kStWarps][NR], s_l[kStWarps][NR];
-  __shared__ __align__(16) float s_o[kStWarps][NR][DH];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int h = blockIdx.x, b = blockIdx.y, chunk_id = blockIdx.z;
   const Kv8Seq s = kv8_seq(a, b, threadIdx.x == 0 && h == 0 && chunk_id == 0);
   const int N = a.rows * a.G, Nv = s.rows * a.G;                  // rows of the call, rows that exist
   const Kv8Split sp = kv8_split_keys(s.len, plan.chunk);
   if (chunk_id >= sp.n) return;
-  const int k0 = chunk_id * sp.per, k1 = min(s.len, k0 + sp.per);
+  const int k0 = chunk_id * sp.per, k1 = min(s.len, k0 + sp.per), n_groups = (k1 - k0 + 15) / 16;
   const bool last = chunk_id == sp.n - 1;
-  for (int i = threadIdx.x; i < (k1 - k0 + 15) / 16; i += kStWarps * 32) s_page[i] = kv8_page(a, s.slot, (k0 + 16 * i) >> a.c.pt_log2);
+  for (int i = threadIdx.x; i < n_groups; i += kStWarps * 32) {
+    const int page = kv8_page(a, s.slot, (k0 + 16 * i) >> a.c.pt_log2);
+    const float sv = fmaxf(a.c.vs[(size_t)page * a.c.hkv + h], kv8_pow2(-100));
+    s_group[i] = make_float4(a.c.ks[(size_t)page * a.c.hkv + h], __log2f(sv), 1.f / sv, __int_as_float(page));
+  }
 
-  // Q fragments: rows g and g + 8, d of this lane in the order of the K words; a power of two brings a row's largest
-  // finite element to [1, 2)
-  uint32_t qa[KW][2], qb[NT == 2 ? KW : 1][2];
-  float crow[NT];
+  // Q as the B operand: row g of each tile, d of this lane in the order of the K words; a power of two brings a row's
+  // largest finite element to [1, 2)
+  uint32_t q[NT][KW][2];
+  float crow[NT][2];                              // of rows 2t, 2t + 1
 #pragma unroll
-  for (int half = 0; half < NT; ++half) {
-    const int i = g + 8 * half;
+  for (int n = 0; n < NT; ++n) {
+    const int i = g + 8 * n;
     const bool on = i < Nv;
-    const bf16* qp = a.q + (size_t)((long long)b * a.rows + (on ? i / a.G : 0)) * a.q_stride + (size_t)(h * a.G + (on ? i % a.G : 0)) * DH + t * (DH / 4);
+    const int r = on ? i / a.G : 0;
+    const bf16* qp = a.q + (size_t)((long long)b * a.rows + r) * a.q_stride + (size_t)(h * a.G + (on ? i - r * a.G : 0)) * DH + t * (DH / 4);
     uint4 raw[DH / 32];
     uint32_t big = 0;
 #pragma unroll
-    for (int e = 0; e < DH / 32; ++e) {
-      raw[e] = on ? *(reinterpret_cast<const uint4*>(qp) + e) : make_uint4(0u, 0u, 0u, 0u);
-      big = kv8_max_finite(big, raw[e]);
-    }
+    for (int e = 0; e < DH / 32; ++e) raw[e] = on ? *(reinterpret_cast<const uint4*>(qp) + e) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int e = 0; e < DH / 32; ++e) big = kv8_max_finite(big, raw[e]);
     big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
     big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
     const int ex = kv8_row_exp(big);
-    crow[half] = a.scale_log2e * kv8_pow2(ex);
-    const float inv = kv8_pow2(-ex);
+    const float c = a.scale_log2e * kv8_pow2(ex), inv = kv8_pow2(-ex);
+    crow[n][0] = __shfl_sync(0xffffffffu, c, 8 * t);
+    crow[n][1] = __shfl_sync(0xffffffffu, c, 8 * t + 4);
 #pragma unroll
     for (int e = 0; e < DH / 32; ++e) {
       uint32_t f[4];
       kv8_bf16x8_to_half(raw[e], inv, f);
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {            // word 2e + w of the K piece: d 4 (2e + w) .. + 3
-        if (half == 0) { qa[2 * e + w][0] = f[2 * w]; qa[2 * e + w][1] = f[2 * w + 1]; }
-        else { qb[NT == 2 ? 2 * e + w : 0][0] = f[2 * w]; qb[NT == 2 ? 2 * e + w : 0][1] = f[2 * w + 1]; }
-      }
+      for (int w = 0; w < 2; ++w) { q[n][2 * e + w][0] = f[2 * w]; q[n][2 * e + w][1] = f[2 * w + 1]; }   // word 2e + w: d 4 (2e + w) .. + 3
     }
   }
   __syncthreads();
@@ -118,101 +130,135 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int n = 0; n < NT; ++n) o[m][n][0] = o[m][n][1] = o[m][n][2] = o[m][n][3] = 0.f;
-  float m_ref[NT], l[NT];
+  float m_ref[NT][2], l[NT][2];                   // of rows 2t, 2t + 1
 #pragma unroll
-  for (int n = 0; n < NT; ++n) { m_ref[n] = -INFINITY; l[n] = 0.f; }
+  for (int n = 0; n < NT; ++n) { m_ref[n][0] = m_ref[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f; }
 
-  // x[n][4]: rows g + 8n, keys 2t, 2t+1, 2t+8, 2t+9, scaled, -inf where hidden.  Turns them into P and returns the B operand.
+  // x[n][4]: (key g, rows 2t, 2t+1), (key g + 8, the same rows), scaled, -inf where hidden.  Turns them into P and returns the
+  // B operand.
   auto weights = [&](float (&x)[NT][4], uint32_t (&pb)[NT][2]) {
     bool up = false;
-    float mt[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      mt[n] = fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3]));
-      up |= mt[n] > m_ref[n] + 8.f;
-    }
+    for (int n = 0; n < NT; ++n) up |= fmaxf(x[n][0], x[n][2]) > m_ref[n][0] + 8.f || fmaxf(x[n][1], x[n][3]) > m_ref[n][1] + 8.f;
     if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float mm = fmaxf(mt[n], __shfl_xor_sync(0xffffffffu, mt[n], 1));
-        mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, 2));
-        const float mn = mm > m_ref[n] + 8.f ? mm : m_ref[n];
-        const float al = mn == m_ref[n] ? 1.f : exp2f(m_ref[n] - mn);       // 0 the first time
-        m_ref[n] = mn;
-        l[n] *= al;
-        const float a0 = __shfl_sync(0xffffffffu, al, 8 * t), a1 = __shfl_sync(0xffffffffu, al, 8 * t + 4);   // rows 2t, 2t + 1
+        float al[2];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) { o[m][n][0] *= a0; o[m][n][1] *= a1; o[m][n][2] *= a0; o[m][n][3] *= a1; }
+        for (int e = 0; e < 2; ++e) {
+          float mm = fmaxf(x[n][e], x[n][2 + e]);
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
+          const float mn = mm > m_ref[n][e] + 8.f ? mm : m_ref[n][e];
+          al[e] = mn == m_ref[n][e] ? 1.f : exp2f(m_ref[n][e] - mn);       // 0 the first time
+          m_ref[n][e] = mn;
+          l[n][e] *= al[e];
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) { o[m][n][0] *= al[0]; o[m][n][1] *= al[1]; o[m][n][2] *= al[0]; o[m][n][3] *= al[1]; }
       }
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float mu = m_ref[n] == -INFINITY ? 0.f : m_ref[n];
+      const float m0 = m_ref[n][0] == -INFINITY ? 0.f : m_ref[n][0], m1 = m_ref[n][1] == -INFINITY ? 0.f : m_ref[n][1];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[n][e] = kv8_ex2(x[n][e] - mu);
+      for (int e = 0; e < 4; ++e) x[n][e] = kv8_ex2(x[n][e] - (e & 1 ? m1 : m0));
       const __half2 p0 = __floats2half2_rn(x[n][0], x[n][1]), p1 = __floats2half2_rn(x[n][2], x[n][3]);
-      pb[n][0] = *reinterpret_cast<const uint32_t*>(&p0);
-      pb[n][1] = *reinterpret_cast<const uint32_t*>(&p1);
+      pb[n][0] = transpose8x8(*reinterpret_cast<const uint32_t*>(&p0));
+      pb[n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&p1));
     }
   };
 
-  struct Scales { float k, v; };
-  auto load = [&](int gi, Group<DH>& w, Scales& sc) {
-    const size_t ph = (size_t)s_page[gi] * a.c.hkv + h;
-    const uint8_t* kb = a.c.k + (ph * a.c.pt + ((k0 + 16 * gi) & (a.c.pt - 1))) * DH;
-    const uint8_t* vb = a.c.v + (kb - a.c.k);
-    sc.k = __ldg(a.c.ks + ph);
-    sc.v = __ldg(a.c.vs + ph);
+  const size_t page_bytes = (size_t)a.c.hkv * a.c.pt * DH;
+  const long long v_off = a.c.v - a.c.k;
+  const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
+  // the copies of a group: 512 bytes of K or of V per instruction
+  uint32_t put[DH / 32];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) load_words(w.k[i], kb + (g + 8 * i) * DH + t * (DH / 4));
+  for (int i = 0; i < DH / 32; ++i) put[i] = st_place<DH>((lane + 32 * i) / (DH / 16), (lane + 32 * i) % (DH / 16));
+  auto request = [&](int gi, int stage) {
+    if (gi < n_groups) {
+      const uint8_t* src = a.c.k + (size_t)__float_as_int(s_group[gi].w) * page_bytes + (h * a.c.pt + ((k0 + 16 * gi) & (a.c.pt - 1))) * DH + lane * 16;
+      const uint32_t dst = ring_s + stage * (2 * kTile);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_words(w.v[i], vb + (2 * t + (i & 1) + 8 * (i >> 1)) * DH + g * (DH / 8));
+      for (int i = 0; i < DH / 32; ++i) cp_async_16(dst + put[i], src + i * 512);
+#pragma unroll
+      for (int i = 0; i < DH / 32; ++i) cp_async_16(dst + kTile + put[i], src + v_off + i * 512);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-
-  const int n_groups = (k1 - k0 + 15) / 16;
-  Group<DH> cur;
-  Scales sc_cur = {0.f, 0.f};
-  if (warp < n_groups) load(warp, cur, sc_cur);
+  uint32_t at_k[2][DH / 64], at_v[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < DH / 64; ++j) at_k[i][j] = st_place<DH>(g + 8 * i, t * (DH / 64) + j);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) at_v[e] = kTile + st_place<DH>(2 * t + (e & 1) + 8 * (e >> 1), g * DH / 128) + (DH == 64 ? (g & 1) * 8 : 0);
+#pragma unroll
+  for (int i = 0; i < kStStages - 1; ++i) request(warp + i * kStWarps, i);
+  int stage = 0;
+#pragma unroll 1
   for (int gi = warp; gi < n_groups; gi += kStWarps) {
-    Group<DH> nxt;
-    Scales sc_nxt = {0.f, 0.f};
-    if (gi + kStWarps < n_groups) load(gi + kStWarps, nxt, sc_nxt);
-    float sc[2][4];
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStStages - 2) : "memory");
+    __syncwarp();                                 // everybody's copies of this group are there, and the stage before it is read
+    request(gi + (kStStages - 1) * kStWarps, stage == 0 ? kStStages - 1 : stage - 1);
+    const unsigned char* tile = ring + stage * (2 * kTile);
+    const float4 sc_cur = s_group[gi];
+    struct { uint32_t k[2][DH / 16], v[4][DH / 32]; } cur;
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-      sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int ks = 0; ks < KW; ++ks) {
-        uint32_t b0, b1;
-        kv8_unpack4<FMT>(cur.k[nt][ks], b0, b1);
-        mma_f16_16816(sc[nt], qa[ks][0], NT == 2 ? qb[NT == 2 ? ks : 0][0] : 0u, qa[ks][1], NT == 2 ? qb[NT == 2 ? ks : 0][1] : 0u, b0, b1);
+      for (int j = 0; j < DH / 64; ++j) {
+        const uint4 w = *reinterpret_cast<const uint4*>(tile + at_k[i][j]);
+        cur.k[i][4 * j] = w.x; cur.k[i][4 * j + 1] = w.y; cur.k[i][4 * j + 2] = w.z; cur.k[i][4 * j + 3] = w.w;
+      }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (DH == 128) {
+        const uint4 w = *reinterpret_cast<const uint4*>(tile + at_v[e]);
+        cur.v[e][0] = w.x; cur.v[e][1] = w.y; cur.v[e][2] = w.z; cur.v[e][3] = w.w;
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(tile + at_v[e]);
+        cur.v[e][0] = w.x; cur.v[e][1] = w.y;
       }
     }
-    const float sv = fmaxf(sc_cur.v, kv8_pow2(-100)), lsv = __log2f(sv), rsv = 1.f / sv;
+    if (++stage == kStStages) stage = 0;
     float x[NT][4];
-    uint32_t pb[NT][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const float cs = crow[n] * sc_cur.k;
+    for (int n = 0; n < NT; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[n][e] = fmaf(sc[e >> 1][2 * n + (e & 1)], cs, lsv);
+    for (int ks = 0; ks < KW; ++ks) {
+      uint32_t a0, a1, a2, a3;
+      kv8_unpack4<FMT>(cur.k[0][ks], a0, a2);
+      kv8_unpack4<FMT>(cur.k[1][ks], a1, a3);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) mma_f16_16816(x[n], a0, a1, a2, a3, q[n][ks][0], q[n][ks][1]);
     }
     const int left = k1 - (k0 + 16 * gi);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float c0 = crow[n][0] * sc_cur.x, c1 = crow[n][1] * sc_cur.x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[n][e] = fmaf(x[n][e], e & 1 ? c1 : c0, sc_cur.y);
+    }
     if (left < 16) {          // keys behind the end: no weight, and whatever their bytes hold reads as zero
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int key = 2 * t + (e & 1) + 8 * (e >> 1);
-        if (key >= left) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n) x[n][e] = -INFINITY;
+        for (int n = 0; n < NT; ++n)
+          if (g + 8 * (e >> 1) >= left) x[n][e] = -INFINITY;
 #pragma unroll
-          for (int w = 0; w < DH / 32; ++w) cur.v[e][w] = 0u;
-        }
+        for (int w = 0; w < DH / 32; ++w)
+          if (2 * t + (e & 1) + 8 * (e >> 1) >= left) cur.v[e][w] = 0u;
       }
     }
+    uint32_t pb[NT][2];
     weights(x, pb);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) l[n] = fmaf((x[n][0] + x[n][1]) + (x[n][2] + x[n][3]), rsv, l[n]);
+    for (int n = 0; n < NT; ++n) {
+      l[n][0] = fmaf(x[n][0] + x[n][2], sc_cur.z, l[n][0]);
+      l[n][1] = fmaf(x[n][1] + x[n][3], sc_cur.z, l[n][1]);
+    }
 #pragma unroll
     for (int w = 0; w < DH / 32; ++w) {
       // bytes j = 4w .. 4w+3 of this lane's d: pairs (key 2t, key 2t + 1) and (2t + 8, 2t + 9)
@@ -227,89 +273,89 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
         mma_f16_16816(o[2 * w + 1][n], a02, a03, a12, a13, pb[n][0], pb[n][1]);
       }
     }
-    cur = nxt;
-    sc_cur = sc_nxt;
   }
 
-  // ---- the new rows (at most 16): one more group, on the last chunk's first warp
+  // ---- the new rows (at most 16): one more group, on the last chunk's first warp, each key divided by a power of two
   if (last && warp == 0 && a.k_new != nullptr && s.rows > 0) {
-    const size_t nb = (size_t)((long long)b * a.rows) * a.new_stride + (size_t)h * DH;
-    float sc[2][4], ksc[4];                      // ksc: scale of keys 2t, 2t+1, 2t+8, 2t+9
+    const bf16* kn = a.k_new + (size_t)((long long)b * a.rows) * a.new_stride + (size_t)h * DH;
+    const bf16* vn = a.v_new + (kn - a.k_new);
+    float x[NT][4], ksc[2];                      // scale of keys g, g + 8
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-      const int y = g + 8 * nt;
-      const bool on = y < s.rows;
-      const bf16* kp = a.k_new + nb + (size_t)(on ? y : 0) * a.new_stride + t * (DH / 4);
-      uint4 raw[DH / 32];
+    for (int n = 0; n < NT; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
+    uint4 raw[2][DH / 32];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bool on = g + 8 * i < s.rows;
+#pragma unroll
+      for (int e = 0; e < DH / 32; ++e)
+        raw[i][e] = on ? *(reinterpret_cast<const uint4*>(kn + (size_t)(g + 8 * i) * a.new_stride + t * (DH / 4)) + e) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
       uint32_t big = 0;
 #pragma unroll
-      for (int e = 0; e < DH / 32; ++e) {
-        raw[e] = on ? *(reinterpret_cast<const uint4*>(kp) + e) : make_uint4(0u, 0u, 0u, 0u);
-        big = kv8_max_finite(big, raw[e]);
-      }
+      for (int e = 0; e < DH / 32; ++e) big = kv8_max_finite(big, raw[i][e]);
       big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
       big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
-      const int ex = kv8_row_exp(big);
-      const float inv = kv8_pow2(-ex);
-      sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+      ksc[i] = kv8_pow2(kv8_row_exp(big));
+    }
 #pragma unroll
-      for (int e = 0; e < DH / 32; ++e) {
-        uint32_t f[4];
-        kv8_bf16x8_to_half(raw[e], inv, f);
+    for (int e = 0; e < DH / 32; ++e) {
+      uint32_t f0[4], f1[4];
+      kv8_bf16x8_to_half(raw[0][e], 1.f / ksc[0], f0);
+      kv8_bf16x8_to_half(raw[1][e], 1.f / ksc[1], f1);
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const int ks = 2 * e + w;
-          mma_f16_16816(sc[nt], qa[ks][0], NT == 2 ? qb[NT == 2 ? ks : 0][0] : 0u, qa[ks][1], NT == 2 ? qb[NT == 2 ? ks : 0][1] : 0u, f[2 * w], f[2 * w + 1]);
-        }
-      }
+      for (int w = 0; w < 2; ++w)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) ksc[2 * nt + e] = kv8_pow2(__shfl_sync(0xffffffffu, ex, (2 * t + e) * 4));
+        for (int n = 0; n < NT; ++n)
+          mma_f16_16816(x[n], f0[2 * w], f1[2 * w], f0[2 * w + 1], f1[2 * w + 1], q[n][2 * e + w][0], q[n][2 * e + w][1]);
     }
     uint32_t vf[4][DH / 16];                     // fp16 pairs of this lane's DH/8 values of its four keys
-    float lsv[4], rsv[4];
+    int ev[4];
     bool odd = false;                            // a value that is not finite
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int y = 2 * t + (e & 1) + 8 * (e >> 1);
       const bool on = y < s.rows;
-      const bf16* vp = a.v_new + nb + (size_t)(on ? y : 0) * a.new_stride + g * (DH / 8);
-      uint4 raw[DH / 64];
+      uint4 rv[DH / 64];
       uint32_t big = 0;
 #pragma unroll
       for (int w = 0; w < DH / 64; ++w) {
-        raw[w] = on ? *(reinterpret_cast<const uint4*>(vp) + w) : make_uint4(0u, 0u, 0u, 0u);
-        odd |= kv8_zero_non_finite(raw[w]);
-        big = kv8_max_finite(big, raw[w]);
+        rv[w] = on ? *(reinterpret_cast<const uint4*>(vn + (size_t)y * a.new_stride + g * (DH / 8)) + w) : make_uint4(0u, 0u, 0u, 0u);
+        odd |= kv8_zero_non_finite(rv[w]);
+        big = kv8_max_finite(big, rv[w]);
       }
 #pragma unroll
-      for (int q = 4; q < 32; q <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, q));
-      const int ex = kv8_row_exp(big);
-      const float inv = kv8_pow2(-ex);
-      lsv[e] = (float)ex;
-      rsv[e] = inv;
+      for (int d = 4; d < 32; d <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, d));
+      ev[e] = kv8_row_exp(big);
 #pragma unroll
       for (int w = 0; w < DH / 64; ++w) {
         uint32_t f[4];
-        kv8_bf16x8_to_half(raw[w], inv, f);
+        kv8_bf16x8_to_half(rv[w], kv8_pow2(-ev[e]), f);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) vf[e][4 * w + q] = f[q];
+        for (int d = 0; d < 4; ++d) vf[e][4 * w + d] = f[d];
       }
     }
-    float x[NT][4];
-    uint32_t pb[NT][2];
+    int evk[2];                                  // of keys g, g + 8: the lanes g / 2 have them
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int e0 = __shfl_sync(0xffffffffu, ev[2 * i], g >> 1), e1 = __shfl_sync(0xffffffffu, ev[2 * i + 1], g >> 1);
+      evk[i] = g & 1 ? e1 : e0;
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = g + 8 * n, y = 2 * t + (e & 1) + 8 * (e >> 1);
+        const int i = 2 * t + (e & 1) + 8 * n, y = g + 8 * (e >> 1);
         const bool see = i < Nv && y < s.rows && kv8_sees(a, b, i / a.G, y);
-        x[n][e] = see ? fmaf(sc[e >> 1][2 * n + (e & 1)], crow[n] * ksc[e], lsv[e]) : -INFINITY;
+        x[n][e] = see ? fmaf(x[n][e], crow[n][e & 1] * ksc[e >> 1], (float)evk[e >> 1]) : -INFINITY;
       }
+    uint32_t pb[NT][2];
     weights(x, pb);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) l[n] = fmaf(x[n][e], rsv[e], l[n]);
+      for (int e = 0; e < 4; ++e) l[n][e & 1] = fmaf(x[n][e], kv8_pow2(-evk[e >> 1]), l[n][e & 1]);
 #pragma unroll
     for (int m = 0; m < MT; ++m) {               // d = g * DH/8 + 2m (A rows g) and + 2m + 1 (rows g + 8)
       const uint32_t w0 = vf[0][m], w1 = vf[1][m], w2 = vf[2][m], w3 = vf[3][m];
@@ -319,6 +365,7 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
                       __byte_perm(w2, w3, 0x7632), pb[n][0], pb[n][1]);
     }
     if (__any_sync(0xffffffffu, odd)) {          // values that are not finite reach exactly the rows that see them
+#pragma unroll 1
       for (int y = 0; y < s.rows; ++y)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -329,21 +376,25 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-              for (int q = 0; q < 2; ++q) {
-                const float v = __bfloat162float(a.v_new[nb + (size_t)y * a.new_stride + g * (DH / 8) + 2 * m + q]);
-                if (!isfinite(v)) o[m][n][2 * q + e] += v;
+              for (int d = 0; d < 2; ++d) {
+                const float v = __bfloat162float(vn[(size_t)y * a.new_stride + g * (DH / 8) + 2 * m + d]);
+                if (!isfinite(v)) o[m][n][2 * d + e] += v;
               }
           }
     }
   }
 
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();                                // the rings are done with: O takes their place
   // ---- the warps' parts, joined in warp order
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
-    l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
-    if (t == 0) { s_m[warp][g + 8 * n] = m_ref[n]; s_l[warp][g + 8 * n] = l[n]; }
-  }
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
+      if (g == 0) { s_m[warp][2 * t + e + 8 * n] = m_ref[n][e]; s_l[warp][2 * t + e + 8 * n] = l[n][e]; }
+    }
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -352,6 +403,7 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
       for (int e = 0; e < 2; ++e)
         *reinterpret_cast<float2*>(&s_o[warp][2 * t + e + 8 * n][g * (DH / 8) + 2 * m]) = make_float2(o[m][n][e], o[m][n][2 + e]);
   __syncthreads();
+#pragma unroll 1
   for (int x = threadIdx.x; x < N * (DH / 4); x += kStWarps * 32) {
     const int i = x / (DH / 4), c4 = x % (DH / 4);
     float M = -INFINITY, L = 0.f;
@@ -445,10 +497,9 @@ __global__ void __launch_bounds__(256) kv8_combine_kernel(const __grid_constant_
 // ---- planning ---------------------------------------------------------------------------------------------------------
 namespace {
 
-// Keys a CTA of the streaming kernel takes.  With few (batch entry, KV head) pairs one wave of CTAs (three to an SM)
+// Keys a CTA of the streaming kernel takes.  With few (batch entry, KV head) pairs one wave of CTAs (four to an SM, two with more than 8 rows)
 // shares the longest sequence evenly; with many, whose lengths differ in a way only the device knows, several waves of
 // shorter parts even them out.  At least 512 keys, so that a CTA's start (page ids, queries, the join) stays a small part.
-constexpr int kStSlots = 148 * 3;
 constexpr int kStMinChunk = 512, kStMaxChunk = 8192;
 int round128(long long x) { return (int)((x + 127) / 128 * 128); }
 
@@ -459,7 +510,7 @@ Kv8Plan make_plan(const Kv8AttnArgs& a, void* workspace) {
   size_t rows, most;                 // partial rows of this call; of any call with a smaller max_len
   if (!p.umma) {
     const long long pairs = (long long)a.batch * a.c.hkv;
-    const long long units = pairs * 4 <= kStSlots ? kStSlots : 6 * kStSlots;
+    const long long slots = 148 * (a.rows * a.G <= 8 ? 4 : 2), units = pairs * 4 <= slots ? slots : 6 * slots;
     const int parts = (int)((units + pairs - 1) / pairs);               // CTAs per pair if every sequence were the longest
     const int longest = round128(((long long)a.max_len + 65534) / 65535);   // the grid's third dimension
     int chunk = round128(((long long)a.max_len + parts - 1) / parts);
@@ -486,7 +537,12 @@ Kv8Plan make_plan(const Kv8AttnArgs& a, void* workspace) {
 
 template <int FMT, int DH, int NT>
 cudaError_t launch_stream(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStream_t st) {
-  kv8_attn_stream_kernel<FMT, DH, NT><<<dim3(a.c.hkv, a.batch, p.max_chunks), kStWarps * 32, p.chunk / 16 * sizeof(int), st>>>(a, p);
+  const auto kernel = kv8_attn_stream_kernel<FMT, DH, NT>;
+  const size_t most = st_body<DH, NT>() + 32768 / 16 * sizeof(float4);           // with the longest chunk there can be
+  const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), most);
+  if (e != cudaSuccess) return e;
+  prefer_max_shared(reinterpret_cast<const void*>(kernel));
+  kernel<<<dim3(a.c.hkv, a.batch, p.max_chunks), kStWarps * 32, st_body<DH, NT>() + p.chunk / 16 * sizeof(float4), st>>>(a, p);
   return cudaGetLastError();
 }
 template <int FMT, int DH>

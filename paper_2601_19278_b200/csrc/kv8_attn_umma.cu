@@ -30,32 +30,17 @@ constexpr int kKuThreads = 640;      // warps 0: producer of K, 1 and 3: MMA iss
 constexpr int kKuPairSlots = 2, kKuSingleSlots = 3;     // 64-key code slots of each ring (K, V): what shared memory leaves
 constexpr int kKuBad = 4096 / 32;
 
-#ifndef KU_RELAX_NS
-#define KU_RELAX_NS 64
-#endif
-#ifndef KU_ISSUE_NS
-#define KU_ISSUE_NS 20
-#endif
-// Bounded wait in little code (the loop is not unrolled: there are some twenty of them); about a second, then the CTA's
-// abort flag is raised and all roles leave.
+// Bounded wait in little code (the loop is not unrolled: there are some twenty of them).  try_wait may suspend the warp,
+// which leaves the issue slots to the softmax warps beside it (1 % of the kernel's time against test_wait, with or without a
+// pause between two looks).  After some seconds the CTA's abort flag is raised and all roles leave.
 __device__ __forceinline__ bool ku_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
 #pragma unroll 1
-  for (int it = 0; it < 16000000; ++it) {
-    if (mbar_test_wait(bar, parity)) return true;
-    if (*abort_flag) return false;
-  }
-  *abort_flag = 1;
-  return false;
-}
-
-// The same for the roles that run ahead of the arithmetic: a pause between two looks.  (Twelve warps that polled without one
-// doubled the time of the softmax warps beside them.)
-__device__ __forceinline__ bool ku_wait_relaxed(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-#pragma unroll 1
   for (int it = 0; it < 4000000; ++it) {
-    if (mbar_test_wait(bar, parity)) return true;
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    if (ok) return true;
     if (*abort_flag) return false;
-    __nanosleep(KU_RELAX_NS);
   }
   *abort_flag = 1;
   return false;
@@ -368,7 +353,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       if (it > 0) {
         if (__any_sync(0xffffffffu, *(volatile int*)&abort_flag != 0)) break;
         if (it > 4000000) { abort_flag = 1; break; }
-        __nanosleep(KU_ISSUE_NS);
+        __nanosleep(20);
       }
     }
    }
@@ -410,7 +395,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
 #pragma unroll 1
     for (int j = 0; j < n && ok; ++j) {
       const int buf = j & 1, use = j >> 1;
-      if (use > 0) ok = ku_wait_relaxed(&empty[buf], (use - 1) & 1, &abort_flag);
+      if (use > 0) ok = ku_wait(&empty[buf], (use - 1) & 1, &abort_flag);
       if (!ok) break;
       if (j < n_cached) {
         if (is_v) {
@@ -425,7 +410,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
 #pragma unroll 1
         for (int q = 0; q < 2; ++q) {        // 64 keys each
           uint8_t* tile = tiles + buf * Ly::tile + q * 8192;
-          ok = ku_wait_relaxed(&c_full[is_v][st], round & 1, &abort_flag);
+          ok = ku_wait(&c_full[is_v][st], round & 1, &abort_flag);
           if (!ok) break;
           const uint8_t* src = ring + st * Ly::slot + ct * 16;
           uint4 w[kUnits];
@@ -566,6 +551,8 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
           uint32_t pk[32];
           float sum = 0.f;
           {
+            // in phases, not element by element: the compiler keeps the order, and 64 exponentials in a row take a warp 600
+            // cycles where the interleaved form took 1000 (the special-function unit's own time is 512)
             float rr[64];
             tmem_ld64(tS + hf * 64, rr);
 #pragma unroll
@@ -573,20 +560,29 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
               const float2 c = scp[g * 16];
               const float mul = crow * c.x, sub = c.y - mu;
               const f32x2 mul2 = pack2(mul, mul), sub2 = pack2(sub, sub);
-              f32x2 ls = pack2(0.f, 0.f);
 #pragma unroll
-              for (int q = 0; q < 16; q += 2) {
-                float x0, x1;
-                unpack2(fma2(pack2(rr[16 * g + q], rr[16 * g + q + 1]), mul2, sub2), x0, x1);
-                const float p0 = kv8_ex2(x0), p1 = kv8_ex2(x1);
-                ls = add2(ls, pack2(p0, p1));
-                const __half2 v2 = __floats2half2_rn(p0, p1);
-                pk[8 * g + q / 2] = *reinterpret_cast<const uint32_t*>(&v2);
+              for (int q = 0; q < 16; q += 2)
+                unpack2(fma2(pack2(rr[16 * g + q], rr[16 * g + q + 1]), mul2, sub2), rr[16 * g + q], rr[16 * g + q + 1]);
+            }
+#pragma unroll
+            for (int q = 0; q < 64; ++q) rr[q] = kv8_ex2(rr[q]);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              f32x2 ls = pack2(rr[16 * g], rr[16 * g + 1]), lt = pack2(rr[16 * g + 2], rr[16 * g + 3]);
+#pragma unroll
+              for (int q = 4; q < 16; q += 4) {
+                ls = add2(ls, pack2(rr[16 * g + q], rr[16 * g + q + 1]));
+                lt = add2(lt, pack2(rr[16 * g + q + 2], rr[16 * g + q + 3]));
               }
               float l0, l1;
-              unpack2(ls, l0, l1);
+              unpack2(add2(ls, lt), l0, l1);
               sum += l0 + l1;
-              l_new = fmaf(l0 + l1, kv8_ex2(-c.y), l_new);      // back to the weights alone
+              l_new = fmaf(l0 + l1, kv8_ex2(-scp[g * 16].y), l_new);      // back to the weights alone
+            }
+#pragma unroll
+            for (int q = 0; q < 32; ++q) {
+              const __half2 v2 = __floats2half2_rn(rr[2 * q], rr[2 * q + 1]);
+              pk[q] = *reinterpret_cast<const uint32_t*>(&v2);
             }
           }
           const bool fine = sum <= 16384.f;
@@ -732,16 +728,17 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
   if (abort_flag && tid == 0) kv8_report(a.status, DEV_TIMEOUT);
 }
 
-// Key steps of a CTA.  Every CTA costs about six steps' worth of start and end (barriers, queries, the first copies, its
-// partial result), a step of one row tile about half a step of two.  Enough CTAs for the GPU at one CTA per SM when there
-// are few, several waves' worth when there are many; never fewer than four steps.
+// Key steps of a CTA.  A CTA's start and end (queries, the first copies, the first scores, its result) cost as much as five or
+// six steps, and a partial result is written, read again and joined, so the keys are split only as far as one wave of
+// CTAs, one to an SM, goes.  (Measured, steps per CTA: 16 ragged sequences of up to 65 steps, 256 cells: 65 steps 169 us, 33: 192,
+// 16: 226; prompt chunk, 256 cells of 44: 44 steps 291 us, 22: 353; one tree, 16 cells of 33 steps: 4 steps 32 us, 3: 37, 8: 38.)
 void kv8_umma_plan(const Kv8AttnArgs& a, Kv8Plan& p) {
   constexpr int kSms = 148, kMinSteps = 4;
   p.n_tiles = (a.rows * a.G + 127) / 128;
   const long long groups = (p.n_tiles + 1) / 2, cells = groups * a.batch * a.c.hkv;
   const int steps = (int)(((long long)a.max_len + 127) / 128) + (a.k_new != nullptr ? (a.rows + 127) / 128 : 0);
   const long long all = ((long long)a.max_len + 127) / 128 + (a.rows + 127) / 128;       // whether or not there are new rows
-  const long long parts = cells >= kSms ? (4 * kSms + cells - 1) / cells : kSms / cells;
+  const long long parts = cells >= kSms ? 1 : kSms / cells;
   long long chunk = (steps + parts - 1) / parts;
   if (chunk < kMinSteps) chunk = kMinSteps;
   const long long longest = all * groups / 63487 + 1;                                     // the grid's third dimension
