@@ -10,24 +10,30 @@
 namespace dart {
 
 // Exponent of the smallest power of two s >= 2^-64 with value <= qmax * s; `bits`: the value's bf16 bits (finite, >= 0).
-__device__ __forceinline__ int kv8_scale_exp(uint32_t bits, int format) {
+template <int FMT>
+__device__ __forceinline__ int kv8_scale_exp(uint32_t bits) {
   const int E = (int)(bits >> 7), M = (int)(bits & 127);
-  const int k = format == KV8_E4M3 ? E - 135 + (M > 96) : E - 133 + (M > 126);   // 448 = 1.75 * 2^8, 127 = 1.984375 * 2^6
+  const int k = FMT == KV8_E4M3 ? E - 135 + (M > 96) : E - 133 + (M > 126);   // 448 = 1.75 * 2^8, 127 = 1.984375 * 2^6
   return max(k, -64);
 }
 
-// Four values to four codes.  e4m3: round to nearest even, saturating; NaN stays NaN.  int8: the same, NaN becomes 0.
-__device__ __forceinline__ uint32_t kv8_pack4(float x0, float x1, float x2, float x3, int format) {
-  if (format == KV8_E4M3) {
+// Four values to four codes.  e4m3: round to nearest even, saturating; NaN stays NaN.  int8: the same (NaN becomes 0), for
+// values of at least -127.5.
+template <int FMT>
+__device__ __forceinline__ uint32_t kv8_pack4(float x0, float x1, float x2, float x3) {
+  if (FMT == KV8_E4M3) {
     const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x0, x1), __NV_SATFINITE, __NV_E4M3);
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x2, x3), __NV_SATFINITE, __NV_E4M3);
-    return lo | (hi << 16);
+    return __byte_perm(lo, hi, 0x5410);
   }
-  auto one = [](float x) { return (uint32_t)(min(max(__float2int_rn(x), -127), 127) & 255); };
-  return one(x0) | (one(x1) << 8) | (one(x2) << 16) | (one(x3) << 24);
+  uint32_t d;
+  asm("{\n.reg .b32 t;\ncvt.pack.sat.s8.s32.b32 t, %4, %3, 0;\ncvt.pack.sat.s8.s32.b32 %0, %2, %1, t;\n}"
+      : "=r"(d) : "r"(__float2int_rn(x0)), "r"(__float2int_rn(x1)), "r"(__float2int_rn(x2)), "r"(__float2int_rn(x3)));
+  return d;
 }
-__device__ __forceinline__ float kv8_value(uint32_t code, int format) {
-  return format == KV8_E4M3 ? __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3))) : (float)(int8_t)code;
+template <int FMT>
+__device__ __forceinline__ float kv8_value(uint32_t code) {
+  return FMT == KV8_E4M3 ? __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3))) : (float)(int8_t)code;
 }
 
 // One team of threads per (layer, batch entry, touched page, KV head, K or V): a warp where a call adds at most 16 rows of
@@ -49,7 +55,7 @@ __device__ __forceinline__ bool team_any(bool x) {
   return TEAM == 32 ? __any_sync(0xffffffffu, x) : __syncthreads_or(x);
 }
 
-template <int DH, int TEAM, int PIECES>
+template <int FMT, int DH, int TEAM, int PIECES>
 __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_constant__ Kv8AppendArgs a) {
   __shared__ uint32_t sh_max[kApThreads / 32];
   constexpr int kPer = DH / 8;                     // pieces of a row
@@ -82,14 +88,19 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
     x.pieces = max(min(a.pt, len + n - first) - x.lo, 0) * kPer;
     if (x.pieces == 0) return;
     x.page = a.table[(size_t)slot * a.max_pages + col];
+    const int j0 = first + x.lo + tid / kPer - len;      // this thread's first row; the next are TEAM / kPer rows apart
+    const bf16* p = src + (size_t)((long long)b * a.rows + j0) * a.row_stride + (tid % kPer) * 8;
+    const size_t step = (size_t)(TEAM / kPer) * a.row_stride;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int e = tid + i * TEAM;
-      if (e < x.pieces) {
-        const int j = first + x.lo + e / kPer - len;
-        int row = a.row_index != nullptr ? a.row_index[(size_t)b * a.max_append + j] : j;
-        if (row < 0 || row >= a.rows) { kv8_report(a.status, KV8_BAD_ARG); row = 0; }
-        x.v[i] = __ldg(reinterpret_cast<const uint4*>(src + (size_t)((long long)b * a.rows + row) * a.row_stride + (e % kPer) * 8));
+      if (tid + i * TEAM < x.pieces) {
+        const bf16* from = p + i * step;
+        if (a.row_index != nullptr) {
+          int row = a.row_index[(size_t)b * a.max_append + j0 + i * (TEAM / kPer)];
+          if (row < 0 || row >= a.rows) { kv8_report(a.status, KV8_BAD_ARG); row = 0; }
+          from = src + (size_t)((long long)b * a.rows + row) * a.row_stride + (tid % kPer) * 8;
+        }
+        x.v[i] = __ldg(reinterpret_cast<const uint4*>(from));
       }
     }
   };
@@ -103,10 +114,22 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
     float* scale = (is_v ? a.vs : a.ks) + ph;
     const bool held = col * a.pt < len;            // the page already holds rows of the sequence
     const float was = held ? *scale : 0.f;
-    uint32_t big = 0;
+    // the largest |x|: bits of both halves of all words, a three-way 16-bit maximum per two words
+    uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i)
-      if (tid + i * TEAM < x.pieces) big = kv8_max_finite(big, x.v[i]);
+      if (tid + i * TEAM < x.pieces) {
+        top = __vimax3_u16x2(top, x.v[i].x & 0x7fff7fffu, x.v[i].y & 0x7fff7fffu);
+        top = __vimax3_u16x2(top, x.v[i].z & 0x7fff7fffu, x.v[i].w & 0x7fff7fffu);
+      }
+    uint32_t big = max(top & 0xffffu, top >> 16);
+    const bool odd = big >= 0x7f80u;               // something is not finite: the largest of the rest, element by element
+    if (odd) {
+      big = 0;
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i)
+        if (tid + i * TEAM < x.pieces) big = kv8_max_finite(big, x.v[i]);
+    }
     big = __reduce_max_sync(0xffffffffu, big);
     if (TEAM > 32) {
       if (lane == 0) sh_max[threadIdx.x >> 5] = big;
@@ -115,7 +138,7 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
       for (int i = 0; i < TEAM / 32; ++i) big = max(big, sh_max[i]);
     }
     team_sync<TEAM>();                             // everybody has read the old scale
-    const float need = kv8_pow2(kv8_scale_exp(big, a.format)), s = fmaxf(need, was);
+    const float need = kv8_pow2(kv8_scale_exp<FMT>(big)), s = fmaxf(need, was);
     const bool exact = (__float_as_uint(s) & 0x7fffffu) == 0u;               // a power of two: the reciprocal is exact
     const float inv = 1.f / s;
 #pragma unroll
@@ -125,16 +148,20 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
         const uint32_t wd[4] = {x.v[i].x, x.v[i].y, x.v[i].z, x.v[i].w};
         float f[8];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) { f[2 * q] = __uint_as_float(wd[q] << 16); f[2 * q + 1] = __uint_as_float(wd[q] & 0xffff0000u); }
-        if (exact) {
+        for (int q = 0; q < 4; ++q) {
+          f[2 * q] = __uint_as_float(wd[q] << 16) * inv;
+          f[2 * q + 1] = __uint_as_float(wd[q] & 0xffff0000u) * inv;
+        }
+        if (!exact || odd) {                       // a scale that is no power of two, or infinities
 #pragma unroll
-          for (int q = 0; q < 8; ++q) f[q] *= inv;
-        } else {
-#pragma unroll
-          for (int q = 0; q < 8; ++q) f[q] = __fdiv_rn(f[q], s);
+          for (int q = 0; q < 8; ++q) {
+            f[q] = __uint_as_float(q & 1 ? wd[q / 2] & 0xffff0000u : wd[q / 2] << 16);
+            f[q] = __fdiv_rn(f[q], s);
+            if (FMT == KV8_INT8 && f[q] < -127.f) f[q] = -127.f;
+          }
         }
         *reinterpret_cast<uint2*>(codes + (size_t)x.lo * DH + (size_t)e * 8) =
-            make_uint2(kv8_pack4(f[0], f[1], f[2], f[3], a.format), kv8_pack4(f[4], f[5], f[6], f[7], a.format));
+            make_uint2(kv8_pack4<FMT>(f[0], f[1], f[2], f[3]), kv8_pack4<FMT>(f[4], f[5], f[6], f[7]));
       }
     }
     if (held && s != was) {          // the page's older codes, to the larger scale
@@ -142,8 +169,8 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
       for (int e = tid; e < x.lo * DH / 4; e += TEAM) {
         uint32_t* c = reinterpret_cast<uint32_t*>(codes) + e;
         const uint32_t o = *c;
-        *c = kv8_pack4(kv8_value(o & 255, a.format) * ratio, kv8_value((o >> 8) & 255, a.format) * ratio,
-                       kv8_value((o >> 16) & 255, a.format) * ratio, kv8_value(o >> 24, a.format) * ratio, a.format);
+        *c = kv8_pack4<FMT>(kv8_value<FMT>(o & 255) * ratio, kv8_value<FMT>((o >> 8) & 255) * ratio, kv8_value<FMT>((o >> 16) & 255) * ratio,
+                            kv8_value<FMT>(o >> 24) * ratio);
       }
     }
     if (tid == 0 && s != was) *scale = s;
@@ -157,25 +184,26 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
 }
 
 namespace {
-template <int DH, int TEAM, int PIECES>
+template <int FMT, int DH, int TEAM, int PIECES>
 cudaError_t launch(const Kv8AppendArgs& a, cudaStream_t st) {
   const long long units = (long long)a.windows * 2 * a.hkv, teams = kApThreads / TEAM;
-  kv8_append_kernel<DH, TEAM, PIECES><<<dim3((unsigned)((units + teams - 1) / teams), a.batch, a.n_layers), kApThreads, 0, st>>>(a);
+  kv8_append_kernel<FMT, DH, TEAM, PIECES><<<dim3((unsigned)((units + teams - 1) / teams), a.batch, a.n_layers), kApThreads, 0, st>>>(a);
   return cudaGetLastError();
 }
-template <int DH>
+template <int FMT, int DH>
 cudaError_t launch_rows(const Kv8AppendArgs& a, cudaStream_t st) {
   const int pieces = (a.max_append < a.pt ? a.max_append : a.pt) * (DH / 8);      // of the fullest page
-  if (pieces <= 32) return launch<DH, 32, 1>(a, st);
-  if (pieces <= 256) return launch<DH, 32, 8>(a, st);
-  if (pieces <= 512) return launch<DH, 256, 2>(a, st);
-  if (pieces <= 1024) return launch<DH, 256, 4>(a, st);
-  return launch<DH, 256, 8>(a, st);
+  if (pieces <= 32) return launch<FMT, DH, 32, 1>(a, st);
+  if (pieces <= 256) return launch<FMT, DH, 32, 8>(a, st);
+  if (pieces <= 512) return launch<FMT, DH, 256, 2>(a, st);
+  if (pieces <= 1024) return launch<FMT, DH, 256, 4>(a, st);
+  return launch<FMT, DH, 256, 8>(a, st);
 }
 }  // namespace
 
 cudaError_t launch_kv8_append(const Kv8AppendArgs& a, cudaStream_t st) {
-  return a.dh == 128 ? launch_rows<128>(a, st) : launch_rows<64>(a, st);
+  if (a.format == KV8_E4M3) return a.dh == 128 ? launch_rows<KV8_E4M3, 128>(a, st) : launch_rows<KV8_E4M3, 64>(a, st);
+  return a.dh == 128 ? launch_rows<KV8_INT8, 128>(a, st) : launch_rows<KV8_INT8, 64>(a, st);
 }
 
 }  // namespace dart

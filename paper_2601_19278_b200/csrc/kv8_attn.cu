@@ -36,7 +36,7 @@ namespace dart {
 // (with rows as M in the first product, half of M empty, and scales and addresses from global memory a group of 4 KB took 319
 // of them and the batch of 64 tokens 120 us): scales, their logarithms and the page ids of the CTA's groups are laid out in
 // shared memory once.
-constexpr int kStWarps = 4, kStStages = 3;
+constexpr int kStWarps = 4, kStStages = 4;
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -69,7 +69,7 @@ constexpr __host__ __device__ int st_body() {
 
 // NT tiles of 8 rows: up to 8 or up to 16 rows.
 template <int FMT, int DH, int NT>
-__global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 4 : 2) kv8_attn_stream_kernel(const __grid_constant__ Kv8AttnArgs a,
+__global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_stream_kernel(const __grid_constant__ Kv8AttnArgs a,
                                                                                         const Kv8Plan plan) {
   constexpr int MT = DH / 16, KW = DH / 16;     // d tiles of the second product; words of a lane's piece of a key
   constexpr int NR = 8 * NT;
@@ -84,9 +84,34 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 4 : 2) kv8_attn_strea
   const Kv8Seq s = kv8_seq(a, b, threadIdx.x == 0 && h == 0 && chunk_id == 0);
   const int N = a.rows * a.G, Nv = s.rows * a.G;                  // rows of the call, rows that exist
   const Kv8Split sp = kv8_split_keys(s.len, plan.chunk);
+  pdl_trigger();                                  // the join may be scheduled as SMs drain; it waits for this grid
   if (chunk_id >= sp.n) return;
   const int k0 = chunk_id * sp.per, k1 = min(s.len, k0 + sp.per), n_groups = (k1 - k0 + 15) / 16;
   const bool last = chunk_id == sp.n - 1;
+  const size_t page_bytes = (size_t)a.c.hkv * a.c.pt * DH;
+  const long long v_off = a.c.v - a.c.k;
+  const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
+  // the copies of a group: 512 bytes of K or of V per instruction
+  uint32_t put[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i) put[i] = st_place<DH>((lane + 32 * i) / (DH / 16), (lane + 32 * i) % (DH / 16));
+  auto request = [&](int gi, int stage, int page) {
+    if (gi < n_groups) {
+      const uint8_t* src = a.c.k + (size_t)page * page_bytes + (h * a.c.pt + ((k0 + 16 * gi) & (a.c.pt - 1))) * DH + lane * 16;
+      const uint32_t dst = ring_s + stage * (2 * kTile);
+#pragma unroll
+      for (int i = 0; i < DH / 32; ++i) cp_async_16(dst + put[i], src + i * 512);
+#pragma unroll
+      for (int i = 0; i < DH / 32; ++i) cp_async_16(dst + kTile + put[i], src + v_off + i * 512);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // the first copies start as soon as their page ids are known, before everything else
+#pragma unroll
+  for (int i = 0; i < kStStages - 1; ++i) {
+    const int gi = warp + i * kStWarps;
+    request(gi, i, gi < n_groups ? kv8_page(a, s.slot, (k0 + 16 * gi) >> a.c.pt_log2) : 0);
+  }
   for (int i = threadIdx.x; i < n_groups; i += kStWarps * 32) {
     const int page = kv8_page(a, s.slot, (k0 + 16 * i) >> a.c.pt_log2);
     const float sv = fmaxf(a.c.vs[(size_t)page * a.c.hkv + h], kv8_pow2(-100));
@@ -169,24 +194,6 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 4 : 2) kv8_attn_strea
     }
   };
 
-  const size_t page_bytes = (size_t)a.c.hkv * a.c.pt * DH;
-  const long long v_off = a.c.v - a.c.k;
-  const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
-  // the copies of a group: 512 bytes of K or of V per instruction
-  uint32_t put[DH / 32];
-#pragma unroll
-  for (int i = 0; i < DH / 32; ++i) put[i] = st_place<DH>((lane + 32 * i) / (DH / 16), (lane + 32 * i) % (DH / 16));
-  auto request = [&](int gi, int stage) {
-    if (gi < n_groups) {
-      const uint8_t* src = a.c.k + (size_t)__float_as_int(s_group[gi].w) * page_bytes + (h * a.c.pt + ((k0 + 16 * gi) & (a.c.pt - 1))) * DH + lane * 16;
-      const uint32_t dst = ring_s + stage * (2 * kTile);
-#pragma unroll
-      for (int i = 0; i < DH / 32; ++i) cp_async_16(dst + put[i], src + i * 512);
-#pragma unroll
-      for (int i = 0; i < DH / 32; ++i) cp_async_16(dst + kTile + put[i], src + v_off + i * 512);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
   uint32_t at_k[2][DH / 64], at_v[4];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -194,14 +201,13 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 4 : 2) kv8_attn_strea
     for (int j = 0; j < DH / 64; ++j) at_k[i][j] = st_place<DH>(g + 8 * i, t * (DH / 64) + j);
 #pragma unroll
   for (int e = 0; e < 4; ++e) at_v[e] = kTile + st_place<DH>(2 * t + (e & 1) + 8 * (e >> 1), g * DH / 128) + (DH == 64 ? (g & 1) * 8 : 0);
-#pragma unroll
-  for (int i = 0; i < kStStages - 1; ++i) request(warp + i * kStWarps, i);
   int stage = 0;
 #pragma unroll 1
   for (int gi = warp; gi < n_groups; gi += kStWarps) {
     asm volatile("cp.async.wait_group %0;" ::"n"(kStStages - 2) : "memory");
     __syncwarp();                                 // everybody's copies of this group are there, and the stage before it is read
-    request(gi + (kStStages - 1) * kStWarps, stage == 0 ? kStStages - 1 : stage - 1);
+    const int ahead = gi + (kStStages - 1) * kStWarps;
+    request(ahead, stage == 0 ? kStStages - 1 : stage - 1, ahead < n_groups ? __float_as_int(s_group[ahead].w) : 0);
     const unsigned char* tile = ring + stage * (2 * kTile);
     const float4 sc_cur = s_group[gi];
     struct { uint32_t k[2][DH / 16], v[4][DH / 32]; } cur;
@@ -497,9 +503,9 @@ __global__ void __launch_bounds__(256) kv8_combine_kernel(const __grid_constant_
 // ---- planning ---------------------------------------------------------------------------------------------------------
 namespace {
 
-// Keys a CTA of the streaming kernel takes.  With few (batch entry, KV head) pairs one wave of CTAs (four to an SM, two with more than 8 rows)
-// shares the longest sequence evenly; with many, whose lengths differ in a way only the device knows, several waves of
-// shorter parts even them out.  At least 512 keys, so that a CTA's start (page ids, queries, the join) stays a small part.
+// Keys a CTA of the streaming kernel takes.  With few (batch entry, KV head) pairs one wave of CTAs (three to an SM, two with more than 8 rows)
+// shares the longest sequence evenly; with many, whose lengths differ in a way only the device knows, two waves of shorter
+// parts even them out (64 ragged sequences: one wave 98.1 us, two 99.8, four 101.7, six 106.7).  At least 512 keys, so that a CTA's start (page ids, queries, the join) stays a small part.
 constexpr int kStMinChunk = 512, kStMaxChunk = 8192;
 int round128(long long x) { return (int)((x + 127) / 128 * 128); }
 
@@ -510,7 +516,7 @@ Kv8Plan make_plan(const Kv8AttnArgs& a, void* workspace) {
   size_t rows, most;                 // partial rows of this call; of any call with a smaller max_len
   if (!p.umma) {
     const long long pairs = (long long)a.batch * a.c.hkv;
-    const long long slots = 148 * (a.rows * a.G <= 8 ? 4 : 2), units = pairs * 4 <= slots ? slots : 6 * slots;
+    const long long slots = 148 * (a.rows * a.G <= 8 ? 3 : 2), units = pairs * 4 <= slots ? slots : 2 * slots;
     const int parts = (int)((units + pairs - 1) / pairs);               // CTAs per pair if every sequence were the longest
     const int longest = round128(((long long)a.max_len + 65534) / 65535);   // the grid's third dimension
     int chunk = round128(((long long)a.max_len + parts - 1) / parts);

@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
   const int groups = (plan.n_tiles + 1) / 2;
   const int group = (int)blockIdx.z % groups, chunk_id = (int)blockIdx.z / groups;
   const Kv8Tiles tl = kv8_tiles(a, plan, s, 2 * group);
+  pdl_trigger();                   // the join may be scheduled as SMs drain; it waits for this grid
   if (chunk_id >= tl.split.n) return;
   const int j0 = chunk_id * tl.split.per, n = min(tl.steps - j0, tl.split.per);     // this CTA's steps j0 .. j0 + n - 1
   const int N = a.rows * a.G, Nv = s.rows * a.G;
