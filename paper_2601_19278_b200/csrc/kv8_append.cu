@@ -44,7 +44,7 @@ __device__ __forceinline__ float kv8_value(uint32_t code) {
 // asks for in a block team (PIECES 16-byte pieces per thread).
 // Measured: 16 x 9 rows x 16 layers x 8 heads 39.0 -> @ACC us with warp teams; 4 x 2047 rows x 8 heads 35.4 -> @PRO us with
 // the reads ahead of the page and registers by page size.
-constexpr int kApThreads = 256;
+constexpr int kApThreads = 128;
 
 template <int TEAM>
 __device__ __forceinline__ void team_sync() {
@@ -195,9 +195,9 @@ cudaError_t launch_rows(const Kv8AppendArgs& a, cudaStream_t st) {
   const int pieces = (a.max_append < a.pt ? a.max_append : a.pt) * (DH / 8);      // of the fullest page
   if (pieces <= 32) return launch<FMT, DH, 32, 1>(a, st);
   if (pieces <= 256) return launch<FMT, DH, 32, 8>(a, st);
-  if (pieces <= 512) return launch<FMT, DH, 256, 2>(a, st);
-  if (pieces <= 1024) return launch<FMT, DH, 256, 4>(a, st);
-  return launch<FMT, DH, 256, 8>(a, st);
+  if (pieces <= 512) return launch<FMT, DH, 128, 4>(a, st);
+  if (pieces <= 1024) return launch<FMT, DH, 128, 8>(a, st);
+  return launch<FMT, DH, 128, 16>(a, st);
 }
 }  // namespace
 
