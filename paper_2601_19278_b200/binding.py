@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional
 
 import numpy as np
@@ -373,23 +374,39 @@ def train_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_l
 
 
 # ---- the target's KV cache in 8 bits, in pages ------------------------------------------------------------------------
-def _kv8_check(t: Optional[torch.Tensor], name: str, dtype, dev: torch.device, shape=None) -> Optional[int]:
-    """Address of a contiguous tensor of this type, device and shape (None stays None); ValueError otherwise."""
+# A call's device time starts at a few microseconds, so the marshalling is kept as short: integer device comparisons, the
+# argument structure packed by one struct.pack (its layout is the C structure's: native alignment), no objects per call.
+_KV8_ATTN = struct.Struct("@7i3P2q7PNP")
+_KV8_APPEND = struct.Struct("@7i2P2q6P")
+_KV8_FN: Dict[str, object] = {}
+_BF16, _I32, _U8 = torch.bfloat16, torch.int32, torch.uint8
+
+
+def _kv8_fn(name: str):
+    fn = _KV8_FN.get(name)
+    if fn is None:
+        fn = _KV8_FN[name] = getattr(lib(), name)
+    return fn
+
+
+def _kv8_check(t: Optional[torch.Tensor], name: str, dtype, dev: int, shape=None) -> int:
+    """Address of a contiguous tensor of this type, device index and shape (0 for None); ValueError otherwise."""
     if t is None:
-        return None
-    if t.dtype != dtype or t.device != dev or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous {dtype} tensor on {dev} is needed, got {t.dtype} on {t.device}"
+        return 0
+    if t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor on cuda:{dev} is needed, got {t.dtype} on {t.device}"
                          f"{'' if t.is_contiguous() else ', not contiguous'}")
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{name}: shape {shape} is needed, got {tuple(t.shape)}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(shape)} is needed, got {tuple(t.shape)}")
     return t.data_ptr()
 
 
-def _kv8_rows(t: torch.Tensor, name: str, heads: int, dim: int, dev: torch.device) -> int:
+def _kv8_rows(t: torch.Tensor, name: str, heads: int, dim: int, dev: int) -> int:
     """Row stride of bf16 [batch, rows, heads, dim] whose heads are packed and whose batch entries are `rows` rows apart."""
-    if t.dtype != torch.bfloat16 or t.device != dev or t.dim() != 4 or t.shape[2] != heads or t.shape[3] != dim:
-        raise ValueError(f"{name}: bf16 [batch, rows, {heads}, {dim}] on {dev} is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    B, R = t.shape[:2]
+    shape = t.shape
+    if t.dtype != _BF16 or t.get_device() != dev or len(shape) != 4 or shape[2] != heads or shape[3] != dim:
+        raise ValueError(f"{name}: bf16 [batch, rows, {heads}, {dim}] on cuda:{dev} is needed, got {t.dtype} {tuple(shape)} on {t.device}")
+    B, R = shape[0], shape[1]
     s0, s1, s2, s3 = t.stride()
     row = s1 if R > 1 else s0 if B > 1 else heads * dim
     if s3 != 1 or (heads > 1 and s2 != dim) or (B > 1 and R > 1 and s0 != R * s1):
@@ -397,13 +414,12 @@ def _kv8_rows(t: torch.Tensor, name: str, heads: int, dim: int, dev: torch.devic
     return row
 
 
-def _kv8_call(fn, name: str, dev: torch.device, stream, *args) -> None:
-    """One call with `dev` current and the stream's handle as its last argument."""
-    if dev.index != torch.cuda.current_device():
+def _kv8_call(name: str, dev: int, stream, *args) -> None:
+    """One call with device `dev` current and the stream's handle as its last argument."""
+    if dev != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
-            return _kv8_call(fn, name, dev, stream, *args)
-    st = stream if stream is not None else torch.cuda.current_stream(dev)
-    rc = fn(*args, st.cuda_stream)
+            return _kv8_call(name, dev, stream, *args)
+    rc = _kv8_fn(name)(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
     if rc != DART_OK:
         raise DartError(rc, name, lib().dart_last_cuda_error(None) if rc == DART_ERR_CUDA else 0)
 
@@ -419,14 +435,15 @@ class Kv8Cache:
         if not k_pages.is_cuda:
             raise ValueError("k_pages must be on a CUDA device (there is no CPU fallback)")
         self.device = k_pages.device
-        shape = tuple(k_pages.shape)
+        self.index = k_pages.get_device()
+        shape = k_pages.shape
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = shape
         self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale    # keep the tensors alive
         self.c = DartKv8Cache(KV8_E4M3 if k_pages.dtype == torch.float8_e4m3fn else KV8_INT8, *shape,
-                              _kv8_check(k_pages, "k_pages", k_pages.dtype, self.device),
-                              _kv8_check(v_pages, "v_pages", k_pages.dtype, self.device, shape),
-                              _kv8_check(k_scale, "k_scale", torch.float32, self.device, shape[:3]),
-                              _kv8_check(v_scale, "v_scale", torch.float32, self.device, shape[:3]))
+                              _kv8_check(k_pages, "k_pages", k_pages.dtype, self.index),
+                              _kv8_check(v_pages, "v_pages", k_pages.dtype, self.index, shape),
+                              _kv8_check(k_scale, "k_scale", torch.float32, self.index, shape[:3]),
+                              _kv8_check(v_scale, "v_scale", torch.float32, self.index, shape[:3]))
         self.ref = C.addressof(self.c)
 
 
@@ -438,13 +455,14 @@ class Kv8Pages:
         if not page_table.is_cuda:
             raise ValueError("page_table must be on a CUDA device (there is no CPU fallback)")
         self.device = page_table.device
+        self.index = page_table.get_device()
         self.page_table, self.seq_lens, self.ref_count = page_table, seq_lens, ref_count
         if page_table.dim() != 2 or ref_count.dim() != 1:
             raise ValueError("page_table [max_seqs, max_pages] and ref_count [n_pages] are needed")
         S, M = page_table.shape
-        self.c = DartKv8Pages(ref_count.shape[0], page_tokens, S, M, _kv8_check(page_table, "page_table", torch.int32, self.device),
-                              _kv8_check(seq_lens, "seq_lens", torch.int32, self.device, (S,)),
-                              _kv8_check(ref_count, "ref_count", torch.int32, self.device))
+        self.c = DartKv8Pages(ref_count.shape[0], page_tokens, S, M, _kv8_check(page_table, "page_table", _I32, self.index),
+                              _kv8_check(seq_lens, "seq_lens", _I32, self.index, (S,)),
+                              _kv8_check(ref_count, "ref_count", _I32, self.index))
         self.ref = C.addressof(self.c)
 
 
@@ -459,15 +477,14 @@ def kv8_attention(cache: Kv8Cache, layer: int, q: torch.Tensor, k_new: Optional[
     """dart_kv8_attention: q, out [batch, rows, n_q_heads, head_dim], k_new, v_new [batch, rows, n_kv_heads, head_dim] bf16 (q and the
     new rows may be slices of one QKV matrix); seq_lens, page_table, slots, n_rows int32 on the device; mask u8
     [batch, rows, rows] (dart_tree_out.mask) or None: causal.  max_len: host bound of the lengths."""
-    dev = cache.device
+    dev = cache.index
     if q.dim() != 4:
         raise ValueError(f"q: [batch, rows, n_q_heads, head_dim] is needed, got {tuple(q.shape)}")
     B, R, H, d = q.shape
     qs = _kv8_rows(q, "q", H, cache.head_dim, dev)
-    kp = vp = None
-    ns = 0
+    kp = vp = ns = 0
     if k_new is not None:
-        if v_new is None or tuple(k_new.shape[:2]) != (B, R) or tuple(v_new.shape[:2]) != (B, R):
+        if v_new is None or k_new.shape[:2] != (B, R) or v_new.shape[:2] != (B, R):
             raise ValueError("k_new and v_new: both [batch, rows, n_kv_heads, head_dim] with q's batch and rows, or neither")
         ns = _kv8_rows(k_new, "k_new", cache.n_kv_heads, d, dev)
         if _kv8_rows(v_new, "v_new", cache.n_kv_heads, d, dev) != ns:
@@ -478,13 +495,12 @@ def kv8_attention(cache: Kv8Cache, layer: int, q: torch.Tensor, k_new: Optional[
     if page_table.dim() != 2:
         raise ValueError("page_table: [max_seqs, max_pages] is needed")
     S, M = page_table.shape
-    i32 = torch.int32
-    a = DartKv8AttnIn(layer, B, R, H, S, M, max_len, q.data_ptr(), kp, vp, qs, ns, _kv8_check(slots, "slots", i32, dev, (B,)),
-                      _kv8_check(seq_lens, "seq_lens", i32, dev, (S,)), _kv8_check(page_table, "page_table", i32, dev),
-                      _kv8_check(n_rows, "n_rows", i32, dev, (B,)), _kv8_check(mask, "mask", torch.uint8, dev, (B, R, R)),
-                      _kv8_check(out, "out", torch.bfloat16, dev, (B, R, H, d)), _kv8_check(workspace, "workspace", torch.uint8, dev),
-                      workspace.numel(), _kv8_check(status, "status", i32, dev))
-    _kv8_call(lib().dart_kv8_attention, "dart_kv8_attention", dev, stream, cache.ref, C.byref(a))
+    a = _KV8_ATTN.pack(layer, B, R, H, S, M, max_len, q.data_ptr(), kp, vp, qs, ns, _kv8_check(slots, "slots", _I32, dev, (B,)),
+                       _kv8_check(seq_lens, "seq_lens", _I32, dev, (S,)), _kv8_check(page_table, "page_table", _I32, dev),
+                       _kv8_check(n_rows, "n_rows", _I32, dev, (B,)), _kv8_check(mask, "mask", _U8, dev, (B, R, R)),
+                       _kv8_check(out, "out", _BF16, dev, (B, R, H, d)), _kv8_check(workspace, "workspace", _U8, dev),
+                       workspace.numel(), _kv8_check(status, "status", _I32, dev))
+    _kv8_call("dart_kv8_attention", dev, stream, cache.ref, a)
 
 
 def kv8_append(cache: Kv8Cache, first_layer: int, k_new: torch.Tensor, v_new: torch.Tensor, seq_lens: torch.Tensor,
@@ -493,53 +509,54 @@ def kv8_append(cache: Kv8Cache, first_layer: int, k_new: torch.Tensor, v_new: to
                stream=None) -> None:
     """dart_kv8_append: k_new, v_new bf16 [n_layers, batch, rows, n_kv_heads, head_dim]; row_index int32 [batch, max_append] (an
     accepted path of dart_tree_verify_inputs) or None: the rows in order.  The caller advances seq_lens."""
-    dev = cache.device
-    if k_new.dim() != 5 or tuple(v_new.shape) != tuple(k_new.shape):
+    dev = cache.index
+    if k_new.dim() != 5 or v_new.shape != k_new.shape:
         raise ValueError("k_new and v_new: [n_layers, batch, rows, n_kv_heads, head_dim] are needed, of one shape")
-    L, B, R = k_new.shape[:3]
+    L, B, R, hkv, d = k_new.shape
     if L < 1:
         raise ValueError("k_new: at least one layer is needed")
-    rs = _kv8_rows(k_new[0], "k_new", cache.n_kv_heads, cache.head_dim, dev)
-    ls = k_new.stride(0) if L > 1 else 0
-    if _kv8_rows(v_new[0], "v_new", cache.n_kv_heads, cache.head_dim, dev) != rs or (L > 1 and v_new.stride(0) != ls):
+    ls, s0, rs, s2, s3 = k_new.stride()
+    if hkv != cache.n_kv_heads or d != cache.head_dim or k_new.dtype != _BF16 or v_new.dtype != _BF16 or k_new.get_device() != dev or \
+            v_new.get_device() != dev:
+        raise ValueError(f"k_new and v_new: bf16 with {cache.n_kv_heads} heads of {cache.head_dim} on cuda:{dev} are needed")
+    if R == 1:
+        rs = s0 if B > 1 else hkv * d
+    if L == 1:
+        ls = 0
+    if s3 != 1 or (hkv > 1 and s2 != d) or (B > 1 and s0 != R * rs):
+        raise ValueError(f"k_new: heads must be packed and batch entries {R} rows apart, got strides {k_new.stride()}")
+    if v_new.stride() != k_new.stride():
         raise ValueError("k_new and v_new must have the same strides")
     if page_table.dim() != 2:
         raise ValueError("page_table: [max_seqs, max_pages] is needed")
     A = max_append if max_append is not None else row_index.shape[1] if row_index is not None else R
     S, M = page_table.shape
-    i32 = torch.int32
-    a = DartKv8AppendIn(first_layer, L, B, R, A, S, M, k_new.data_ptr(), v_new.data_ptr(), rs, ls, _kv8_check(slots, "slots", i32, dev, (B,)),
-                        _kv8_check(seq_lens, "seq_lens", i32, dev, (S,)), _kv8_check(page_table, "page_table", i32, dev),
-                        _kv8_check(n_append, "n_append", i32, dev, (B,)), _kv8_check(row_index, "row_index", i32, dev, (B, A)),
-                        _kv8_check(status, "status", i32, dev))
-    _kv8_call(lib().dart_kv8_append, "dart_kv8_append", dev, stream, cache.ref, C.byref(a))
+    a = _KV8_APPEND.pack(first_layer, L, B, R, A, S, M, k_new.data_ptr(), v_new.data_ptr(), rs, ls, _kv8_check(slots, "slots", _I32, dev, (B,)),
+                         _kv8_check(seq_lens, "seq_lens", _I32, dev, (S,)), _kv8_check(page_table, "page_table", _I32, dev),
+                         _kv8_check(n_append, "n_append", _I32, dev, (B,)), _kv8_check(row_index, "row_index", _I32, dev, (B, A)),
+                         _kv8_check(status, "status", _I32, dev))
+    _kv8_call("dart_kv8_append", dev, stream, cache.ref, a)
 
 
 def kv8_pages_workspace_bytes(pages: Kv8Pages) -> int:
     return lib().dart_kv8_pages_workspace_bytes(pages.ref)
 
 
-def _kv8_lists(dev: torch.device, **lists: torch.Tensor):
-    n = next(iter(lists.values())).numel()
-    return [_kv8_check(t, name, torch.int32, dev, (n,)) for name, t in lists.items()] + [n]
-
-
 def kv8_fork(pages: Kv8Pages, src: torch.Tensor, dst: torch.Tensor, *, status: Optional[torch.Tensor] = None, stream=None) -> None:
     """dart_kv8_fork: slot dst[i] becomes a copy of slot src[i] (shared pages)."""
-    sp, dp, n = _kv8_lists(pages.device, src=src, dst=dst)
-    _kv8_call(lib().dart_kv8_fork, "dart_kv8_fork", pages.device, stream, pages.ref, sp, dp, n,
-              _kv8_check(status, "status", torch.int32, pages.device))
+    dev, n = pages.index, src.numel()
+    _kv8_call("dart_kv8_fork", dev, stream, pages.ref, _kv8_check(src, "src", _I32, dev, (n,)), _kv8_check(dst, "dst", _I32, dev, (n,)), n,
+              _kv8_check(status, "status", _I32, dev))
 
 
 def kv8_release(pages: Kv8Pages, seqs: torch.Tensor, *, status: Optional[torch.Tensor] = None, stream=None) -> None:
     """dart_kv8_release: the slots give back all their pages."""
-    sp, n = _kv8_lists(pages.device, seqs=seqs)
-    _kv8_call(lib().dart_kv8_release, "dart_kv8_release", pages.device, stream, pages.ref, sp, n,
-              _kv8_check(status, "status", torch.int32, pages.device))
+    dev, n = pages.index, seqs.numel()
+    _kv8_call("dart_kv8_release", dev, stream, pages.ref, _kv8_check(seqs, "seqs", _I32, dev, (n,)), n, _kv8_check(status, "status", _I32, dev))
 
 
 def _kv8_same_pool(pages: Kv8Pages, cache: Kv8Cache) -> None:
-    if cache.device != pages.device:
+    if cache.index != pages.index:
         raise ValueError("the cache and its bookkeeping must be on one device")
 
 
@@ -547,19 +564,19 @@ def kv8_reserve(pages: Kv8Pages, cache: Kv8Cache, seqs: torch.Tensor, n_new: tor
                 status: Optional[torch.Tensor] = None, stream=None) -> None:
     """dart_kv8_reserve: pages for the next n_new[i] positions of slot seqs[i]; shared ones are replaced by copies."""
     _kv8_same_pool(pages, cache)
-    sp, np_, n = _kv8_lists(pages.device, seqs=seqs, n_new=n_new)
-    _kv8_call(lib().dart_kv8_reserve, "dart_kv8_reserve", pages.device, stream, pages.ref, cache.ref, sp, np_, n,
-              _kv8_check(workspace, "workspace", torch.uint8, pages.device), workspace.numel(),
-              _kv8_check(status, "status", torch.int32, pages.device))
+    dev, n = pages.index, seqs.numel()
+    _kv8_call("dart_kv8_reserve", dev, stream, pages.ref, cache.ref, _kv8_check(seqs, "seqs", _I32, dev, (n,)),
+              _kv8_check(n_new, "n_new", _I32, dev, (n,)), n, _kv8_check(workspace, "workspace", _U8, dev), workspace.numel(),
+              _kv8_check(status, "status", _I32, dev))
 
 
 def kv8_compact(pages: Kv8Pages, cache: Kv8Cache, *, workspace: torch.Tensor, n_live: Optional[torch.Tensor] = None,
                 status: Optional[torch.Tensor] = None, stream=None) -> None:
     """dart_kv8_compact: the pages in use move to the front of the pool."""
     _kv8_same_pool(pages, cache)
-    _kv8_call(lib().dart_kv8_compact, "dart_kv8_compact", pages.device, stream, pages.ref, cache.ref,
-              _kv8_check(n_live, "n_live", torch.int32, pages.device), _kv8_check(workspace, "workspace", torch.uint8, pages.device),
-              workspace.numel(), _kv8_check(status, "status", torch.int32, pages.device))
+    dev = pages.index
+    _kv8_call("dart_kv8_compact", dev, stream, pages.ref, cache.ref, _kv8_check(n_live, "n_live", _I32, dev),
+              _kv8_check(workspace, "workspace", _U8, dev), workspace.numel(), _kv8_check(status, "status", _I32, dev))
 
 
 def workspace_bytes(cfg: DartConfig) -> int:

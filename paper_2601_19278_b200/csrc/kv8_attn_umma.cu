@@ -367,14 +367,10 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
     const uint8_t* const ring = sC + is_v * n_slots * Ly::slot;
     uint8_t* const tiles = is_v ? sV : sK;
     uint64_t *const full = is_v ? v_full : k_full, *const empty = is_v ? v_empty : k_empty;
-    // 16 codes = two operand chunks per thread and access.  The second 64 columns of a row lie 16 KB further on, in the same
-    // banks: there the two chunks are stored in the other order, and a quarter warp's stores meet eight different bank
-    // groups.  A thread's rows are 16 or 32 apart: one swizzle for all of them.
-    constexpr int kUnits = DH / 32, kLanes = DH / 16, kRowsPerIt = 128 / kLanes;      // per thread; threads per row
-    const int row_in = ct / kLanes, c = 2 * (ct % kLanes);
-    const bool swap = DH == 128 && c >= 8;
-    const uint32_t d0 = (c >> 3) * 16384 + row_in * 128 + ((((c & 7) + (swap ? 1 : 0)) ^ (row_in & 7)) << 4);
-    const uint32_t d1 = (c >> 3) * 16384 + row_in * 128 + ((((c & 7) + (swap ? 0 : 1)) ^ (row_in & 7)) << 4);
+    // Eight threads per row, each with 8 codes (an operand chunk) of the row's first 64 and 8 of its second: eight
+    // neighbouring threads read 64 bytes in a row and write eight chunks in different banks.  16 rows at a time: one swizzle.
+    const int row_in = ct >> 3;
+    const uint32_t from = row_in * DH + (ct & 7) * 8, into = row_in * 128 + (((ct & 7) ^ (row_in & 7)) << 4);
     auto publish = [&](uint64_t* bar) {
       fence_async_smem();
       __syncwarp();
@@ -413,25 +409,31 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
           uint8_t* tile = tiles + buf * Ly::tile + q * 8192;
           ok = ku_wait(&c_full[is_v][st], round & 1, &abort_flag);
           if (!ok) break;
-          const uint8_t* src = ring + st * Ly::slot + ct * 16;
-          uint4 w[kUnits];
+          const uint8_t* src = ring + st * Ly::slot + from;
+          uint2 w[4][DH / 64];
 #pragma unroll
-          for (int it = 0; it < kUnits; ++it) w[it] = *reinterpret_cast<const uint4*>(src + it * 2048);
+          for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int c = 0; c < DH / 64; ++c) w[it][c] = *reinterpret_cast<const uint2*>(src + it * 16 * DH + c * 64);
           __syncwarp();
           if (lane == 0) mbar_arrive(&c_empty[is_v][st]);
           if (++st == n_slots) { st = 0; ++round; }
+          if (valid < 128) {                 // the end of the cache: code 0 is zero in both formats
 #pragma unroll
-          for (int it = 0; it < kUnits; ++it) {
-            const bool live = q * 64 + row_in + it * kRowsPerIt < valid;
-            const uint32_t x0 = swap ? w[it].z : w[it].x, x1 = swap ? w[it].w : w[it].y, x2 = swap ? w[it].x : w[it].z, x3 = swap ? w[it].y : w[it].w;
-            uint4 f, g;
-            kv8_unpack4<FMT>(live ? x0 : 0u, f.x, f.y);      // code 0 is zero in both formats
-            kv8_unpack4<FMT>(live ? x1 : 0u, f.z, f.w);
-            kv8_unpack4<FMT>(live ? x2 : 0u, g.x, g.y);
-            kv8_unpack4<FMT>(live ? x3 : 0u, g.z, g.w);
-            *reinterpret_cast<uint4*>(tile + d0 + it * kRowsPerIt * 128) = f;
-            *reinterpret_cast<uint4*>(tile + d1 + it * kRowsPerIt * 128) = g;
+            for (int it = 0; it < 4; ++it)
+              if (q * 64 + row_in + it * 16 >= valid)
+#pragma unroll
+                for (int c = 0; c < DH / 64; ++c) w[it][c] = make_uint2(0u, 0u);
           }
+#pragma unroll
+          for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int c = 0; c < DH / 64; ++c) {
+              uint4 f;
+              kv8_unpack4<FMT>(w[it][c].x, f.x, f.y);
+              kv8_unpack4<FMT>(w[it][c].y, f.z, f.w);
+              *reinterpret_cast<uint4*>(tile + into + it * 2048 + c * 16384) = f;
+            }
         }
         if (!ok) break;
         publish(&full[buf]);

@@ -133,6 +133,14 @@ def test_struct_layouts_match_the_header(b, tmp_path):
     assert [int(x) for x in subprocess.check_output([str(exe)]).split()] == want
 
 
+def test_packed_arguments_are_the_structures(b):
+    for packer, s in ((b._KV8_ATTN, b.DartKv8AttnIn), (b._KV8_APPEND, b.DartKv8AppendIn)):
+        assert packer.size == C.sizeof(s)
+        values = list(range(1, len(s._fields_) + 1))
+        filled = s.from_buffer_copy(packer.pack(*values))
+        assert [getattr(filled, f[0]) for f in s._fields_] == values
+
+
 def test_the_binding_refuses_host_tensors(b):
     pages = torch.zeros(1, 4, 2, 16, 64, dtype=torch.int8)
     scale = torch.ones(1, 4, 2)
