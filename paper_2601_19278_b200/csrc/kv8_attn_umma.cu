@@ -114,8 +114,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// Registers per thread of a warpgroup from here on (the kernel is launched with 96): softmax 144 x 256 threads,
-// converters 64 x 256, the rest 64 x 128, together the 61440 the block was launched with.
+// Registers per thread of a warpgroup from here on (the kernel is launched with 96): softmax 136 x 256 threads,
+// converters 72 x 256, the rest 64 x 128, together the 61440 the block was launched with.
 template <int N>
 __device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -192,7 +192,12 @@ __device__ __forceinline__ void bulk_prefetch(const void* src, uint32_t bytes) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
 
-template <int FMT, int DH>
+// Whether all rows of the warp that exist see new row y (causal).
+__device__ __forceinline__ bool ku_all_see(int r, bool on, int rows, int y) { return y < rows && __all_sync(0xffffffffu, !on || y <= r); }
+
+// CHUNK: a prompt's chunk, whose new rows fill key steps that all rows of a tile see; they have a path of their own, which trees and
+// few rows do without (it costs the cached steps beside it a sixth: registers).
+template <int FMT, int DH, bool CHUNK>
 __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __grid_constant__ Kv8AttnArgs a, const Kv8Plan plan) {
   using Ly = KuLayout<DH>;
   extern __shared__ __align__(1024) uint8_t sm[];
@@ -208,7 +213,8 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
   const Kv8Seq s = kv8_seq(a, b, tid == 0 && h == 0 && blockIdx.z == 0);
   // unit -> (group of row tiles, chunk): chunk-major, so that the full chunks of all sequences start first
   const int groups = (plan.n_tiles + 1) / 2;
-  const int group = (int)blockIdx.z % groups, chunk_id = (int)blockIdx.z / groups;
+  // (and the heavier groups: of a chunk the last rows, which see most; else the pairs before a single tile)
+  const int nth = (int)blockIdx.z % groups, group = CHUNK ? groups - 1 - nth : nth, chunk_id = (int)blockIdx.z / groups;
   const Kv8Tiles tl = kv8_tiles(a, plan, s, 2 * group);
   pdl_trigger();                   // the join may be scheduled as SMs drain; it waits for this grid
   if (chunk_id >= tl.split.n) return;
@@ -359,7 +365,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
     }
    }
   } else if (warp >= 12) {
-    reg_dec<64>();
+    reg_dec<72>();
     // ---- converters: codes (or new rows) to fp16 operand tiles
     // (the first four warps K, the others V and the scales: a key per thread, page id two steps and scales one step ahead)
     const int is_v = (warp - 12) >> 2, ct = (tid - 384) & 127, cw = warp & 3;
@@ -457,18 +463,18 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       }
     }
   } else {
-    reg_inc<144>();
+    reg_inc<136>();
     // ---- softmax of pipeline p: thread = row of its tile = tensor-memory lane
     const int p = (warp - 4) >> 2, wq = warp & 3, row = wq * 32 + lane, np = steps_of(p);
     const int tile = tl.first + (pair ? p : 0), i_row = tile * 128 + row;
     const bool on = i_row < Nv;
-    const int r = i_row / a.G, g_head = h * a.G + i_row - r * a.G;       // (of rows that exist)
+    const int r = i_row / a.G;            // (of rows that exist)
     const uint32_t tS = tmem + ((uint32_t)(wq * 32) << 16) + p * 256, tO = tS + 128;
     float crow = 0.f;
     if (pair || p == 0) {
       float inv;
       int ex;
-      ku_row_to_operand<DH>(a.q + (on ? (size_t)((long long)b * a.rows + r) * a.q_stride + (size_t)g_head * DH : 0), on,
+      ku_row_to_operand<DH>(a.q + (on ? (size_t)((long long)b * a.rows + r) * a.q_stride + (size_t)(h * a.G + i_row - r * a.G) * DH : 0), on,
                             sQ + (pair ? p : 0) * Ly::tile, row, false, inv, ex);
       crow = a.scale_log2e * kv8_pow2(ex);
       if (!pair) s_ml[0][row].x = crow;
@@ -524,6 +530,35 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
           }
           tmem_st_wait();
         }
+        return true;
+      };
+      // New rows in one pass against the reference so far, a scale per key; false: a weight was too large, nothing is written.
+      auto new_rows_pass = [&]() -> bool {
+        const float mu = m_ref == -INFINITY ? 0.f : m_ref;
+        float sum0 = 0.f, sum1 = 0.f, w0 = 0.f, w1 = 0.f;
+        uint32_t pk[32];
+#pragma unroll
+        for (int c0 = 0; c0 < 64; c0 += 16) {
+          uint32_t rr[16];
+          tmem_ld16(tS + hf * 64 + c0, rr);
+          tmem_ld_wait();
+#pragma unroll
+          for (int q = 0; q < 16; q += 2) {
+            const float4 c = *reinterpret_cast<const float4*>(scp + c0 + q);      // two keys
+            const float p0 = kv8_ex2(fmaf(__uint_as_float(rr[q]), crow * c.x, c.y - mu));
+            const float p1 = kv8_ex2(fmaf(__uint_as_float(rr[q + 1]), crow * c.z, c.w - mu));
+            sum0 += p0;
+            sum1 += p1;
+            w0 = fmaf(p0, kv8_ex2(-c.y), w0);
+            w1 = fmaf(p1, kv8_ex2(-c.w), w1);
+            const __half2 v2 = __floats2half2_rn(p0, p1);
+            pk[(c0 + q) / 2] = *reinterpret_cast<const uint32_t*>(&v2);
+          }
+        }
+        const bool fine = !on || (sum0 + sum1 <= 16384.f && m_ref != -INFINITY);
+        if (__any_sync(0xffffffffu, !fine)) return false;
+        l += w0 + w1;
+        tmem_st32(tS + hf * 64, pk);
         return true;
       };
       if (cached && left >= 128) {
@@ -597,8 +632,11 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
           first = true;
         }
         if (!ok) break;
+      } else if (CHUNK && x > 0 && !cached && ku_all_see(r, on, s.rows, ((j0 + j - tl.cached) << 7) + hf * 64 + 63) &&
+                 new_rows_pass()) {
+        // 64 new rows that every row of the warp sees
       } else {
-        // the end of the cache, or new rows with a scale per key: 16 columns at a time, twice, in little code
+        // the end of the cache, or new rows that some rows do not see: 16 columns at a time, twice, in little code
         int hi;                           // last visible column, if they are a prefix
         if (cached) hi = left - 1 - hf * 64;
         else hi = min(r, s.rows - 1) - ((j0 + j - tl.cached) << 7) - hf * 64;
@@ -678,7 +716,10 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       }
       const int c_lo = pair ? 0 : p * (DH / 2), c_hi = pair ? DH : c_lo + DH / 2;
       const size_t part = (((size_t)(b * a.c.hkv + h) * plan.n_tiles + tile) * plan.max_chunks + chunk_id) * 128 + row;
-      bf16* out = a.out + ((size_t)((long long)b * a.rows + r) * a.hq + g_head) * DH;
+      int G = a.G;                        // (opaque: the row's place is worked out again instead of kept in registers through the loop)
+      asm volatile("" : "+r"(G));
+      const int r_out = i_row / G;
+      bf16* out = a.out + ((size_t)((long long)b * a.rows + r_out) * a.hq + h * G + i_row - r_out * G) * DH;
       const bool bad = sh.any_bad != 0 && on;
 #pragma unroll 1
       for (int cb = c_lo; cb < c_hi; cb += 8) {
@@ -695,7 +736,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
         if (bad) {                        // values that are not finite reach exactly the rows that see them
 #pragma unroll 1
           for (int y = 0; y < s.rows; ++y) {
-            if (!((s_bad[y >> 5] >> (y & 31)) & 1u) || !kv8_sees(a, b, r, y)) continue;
+            if (!((s_bad[y >> 5] >> (y & 31)) & 1u) || !kv8_sees(a, b, r_out, y)) continue;
             const uint4 v = *reinterpret_cast<const uint4*>(a.v_new + (size_t)((long long)b * a.rows + y) * a.new_stride + (size_t)h * DH + cb);
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -755,13 +796,17 @@ void kv8_umma_plan(const Kv8AttnArgs& a, Kv8Plan& p) {
 }
 
 namespace {
-template <int FMT, int DH>
-cudaError_t launch(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStream_t st) {
-  const auto kernel = kv8_attn_umma_kernel<FMT, DH>;
+template <int FMT, int DH, bool CHUNK>
+cudaError_t launch_kernel(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStream_t st) {
+  const auto kernel = kv8_attn_umma_kernel<FMT, DH, CHUNK>;
   const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), KuLayout<DH>::smem);
   if (e != cudaSuccess) return e;
   kernel<<<dim3(a.c.hkv, a.batch, (p.n_tiles + 1) / 2 * p.max_chunks), kKuThreads, KuLayout<DH>::smem, st>>>(a, p);
   return cudaGetLastError();
+}
+template <int FMT, int DH>
+cudaError_t launch(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStream_t st) {
+  return a.mask == nullptr && a.k_new != nullptr && a.rows > 128 ? launch_kernel<FMT, DH, true>(a, p, st) : launch_kernel<FMT, DH, false>(a, p, st);
 }
 }  // namespace
 
