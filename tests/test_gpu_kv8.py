@@ -272,6 +272,86 @@ def test_bad_lengths_slots_counts_and_pages_are_reported(R):
     torch.testing.assert_close(attend(c, 0, q, kn, vn, 90, table=table), good, rtol=0, atol=0)
 
 
+@pytest.mark.parametrize("R,H,hkv,big", [(400, 1, 1, 1.0), (400, 2, 2, 25.0), (300, 3, 1, 0.01)])
+def test_prompt_chunks_whose_new_rows_dominate(R, H, hkv, big):
+    """Key steps of new rows that whole tiles see, with scores that grow along the chunk (the reference maximum moves in
+    the middle of it) and with a cache of a few keys or none."""
+    c = Case([0, 3, 140], 16, "e4m3", hkv, 128, seed=R)
+    q, kn, vn = c.bf16(3, R, H, 128), c.bf16(3, R, hkv, 128), c.bf16(3, R, hkv, 128)
+    kn *= torch.linspace(0.1, big, R).view(1, R, 1, 1)
+    vn *= torch.exp2(torch.randint(-6, 7, (1, R, 1, 1)).float())
+    got = attend(c, 0, q.to(DEV), kn.to(DEV), vn.to(DEV), 140)
+    check(c, 0, got, q, kn, vn, only=[0, 1, 63, 64, 127, 128, 129, 191, 192, 255, 256, 257, R - 1])
+
+
+def test_pools_past_four_gigabytes():
+    """Pages whose bytes lie beyond 32-bit offsets: append into them, read them back by attention on both kernels, copy them."""
+    hkv, pt, d, n_pages = 8, 64, 128, 75000                       # 4.9 GB each of K and V
+    k, v = (torch.empty(1, n_pages, hkv, pt, d, dtype=torch.int8, device=DEV) for _ in range(2))
+    ks, vs = (torch.full((1, n_pages, hkv), float("nan"), device=DEV) for _ in range(2))
+    cache = b.Kv8Cache(k, v, ks, vs)
+    rng = np.random.default_rng(0)
+    ref = torch.ones(n_pages, dtype=torch.int32, device=DEV)      # everything taken but the last pages
+    ref[-6:] = 0
+    table = torch.full((2, 4), -1, dtype=torch.int32, device=DEV)
+    lens = torch.zeros(2, dtype=torch.int32, device=DEV)
+    pages = b.Kv8Pages(table, lens, ref, pt)
+    ws = torch.empty(b.kv8_pages_workspace_bytes(pages), dtype=torch.uint8, device=DEV)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    status = i32(0)
+    b.kv8_reserve(pages, cache, i32(0), i32(150), workspace=ws, status=status)
+    assert table[0, :3].tolist() == [n_pages - 6, n_pages - 5, n_pages - 4]
+    rows = [torch.from_numpy(rng.standard_normal((1, 1, 150, hkv, d)).astype(np.float32)).to(torch.bfloat16) for _ in range(2)]
+    b.kv8_append(cache, 0, rows[0].to(DEV), rows[1].to(DEV), lens, table, slots=i32(0), status=status)
+    lens[0] = 150
+    b.kv8_fork(pages, i32(0), i32(1), status=status)
+    b.kv8_reserve(pages, cache, i32(1), i32(4), workspace=ws, status=status)           # the last page is copied
+    assert table[1].tolist() == [n_pages - 6, n_pages - 5, n_pages - 3, -1] and int(status) == 0
+    codes = [np.zeros((1, 4, hkv, pt, d), np.uint8) for _ in range(2)]
+    pool = ok.Pool(codes, [np.ones((1, 4, hkv)) for _ in range(2)], "int8")
+    pool.append(0, [0, 1, 2], 0, rows[0][0, 0].double().numpy(), rows[1][0, 0].double().numpy())
+    for R in (1, 20):
+        q, kn, vn = (torch.from_numpy(rng.standard_normal((2, R, h, d)).astype(np.float32)).to(torch.bfloat16) for h in (2 * hkv, hkv, hkv))
+        out = torch.empty(2, R, 2 * hkv, d, dtype=torch.bfloat16, device=DEV)
+        w = torch.empty(b.kv8_attention_workspace_bytes(cache, 2, R, 2 * hkv, 256), dtype=torch.uint8, device=DEV)
+        b.kv8_attention(cache, 0, q.to(DEV), kn.to(DEV), vn.to(DEV), lens, table, out, max_len=256, workspace=w, status=status)
+        for i in range(2):
+            want, absv, absx = ok.attention(pool, 0, [0, 1, 2], 150, q[i].double().numpy(), kn[i].double().numpy(), vn[i].double().numpy(), None)
+            tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -10 + 2.0 ** -18 * absx[..., None]) * absv + 2.0 ** -18
+            assert np.all(np.abs(out[i].double().cpu().numpy() - want) <= tol)
+    ref[:-6] = 0                                                  # only the two sequences live: they move to the front
+    b.kv8_compact(pages, cache, workspace=ws, status=status)
+    b.kv8_attention(cache, 0, q.to(DEV), kn.to(DEV), vn.to(DEV), lens, table, out, max_len=256, workspace=w, status=status)
+    assert table[0, :3].tolist() == [0, 1, 2] or sorted(table[0, :3].tolist() + [int(table[1, 2])]) == [0, 1, 2, 3]
+    assert np.all(np.abs(out[1].double().cpu().numpy() - want) <= tol) and int(status) == 0
+
+
+def test_other_streams_and_first_calls_inside_a_capture():
+    """A call on a stream that is not the current one, and page operations captured and replayed."""
+    s = Server(40, 16, 6, 6, seed=31)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    b.kv8_reserve(s.pages, s.cache, s.i32([0, 1]), s.i32([20, 30]), workspace=s.ws, status=s.status, stream=st)
+    s.copies(s.book.reserve([0, 1], [20, 30]))
+    st.synchronize()
+    s.advance([0, 1], [20, 30])
+    s.check()
+    src, dst, who, more = s.i32([0, 1]), s.i32([2, 3]), s.i32([0, 1, 2, 3]), s.i32([1, 1, 1, 1])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        b.kv8_fork(s.pages, src, dst, status=s.status)
+        b.kv8_reserve(s.pages, s.cache, who, more, workspace=s.ws, status=s.status)
+        b.kv8_release(s.pages, who[2:], status=s.status)
+        b.kv8_compact(s.pages, s.cache, workspace=s.ws, n_live=s.n_live, status=s.status)
+    for _ in range(3):
+        g.replay()
+        s.book.fork([0, 1], [2, 3])
+        s.copies(s.book.reserve([0, 1, 2, 3], [1, 1, 1, 1]))
+        s.book.release([2, 3])
+        s.copies(s.book.compact())
+        s.check()
+
+
 def test_results_repeat_bit_for_bit():
     c = Case([5000, 1200, 77], 64, "e4m3", 2, 128, seed=13)
     for R in (1, 3, 60):
