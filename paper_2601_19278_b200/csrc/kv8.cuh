@@ -55,9 +55,10 @@ struct Kv8PoolArgs {
 // How a call of the attention is cut into CTAs (launch_kv8_attention).
 struct Kv8Plan {
   int umma;              // rows on tcgen05 (kv8_attn_umma.cu) instead of the streaming kernel
-  int chunk;             // stream: keys a CTA takes at most; umma: 128-key steps of a CTA with two row tiles
+  int chunk;             // stream: keys a CTA takes at most; umma: its 128-key steps (beside pairs, a single tile's CTA takes twice as many)
   int max_chunks;        // CTAs that may share a (batch entry, KV head, row tile)
-  int n_tiles;           // umma: 128-row tiles; tiles 2p and 2p + 1 go together, an odd last one alone
+  int n_tiles;           // umma: 128-row tiles
+  int paired;            // tiles 2p and 2p + 1 go together, an odd last one alone; else every tile alone
   float *o_part, *ml_part;
   size_t bytes;          // of workspace
 };
@@ -116,13 +117,13 @@ __device__ __forceinline__ int kv8_page(const Kv8AttnArgs& a, int slot, int col)
 struct Kv8Tiles { int first, count, cached, steps; Kv8Split split; };      // first tile and number of tiles of the group
 __device__ __forceinline__ Kv8Tiles kv8_tiles(const Kv8AttnArgs& a, const Kv8Plan& plan, const Kv8Seq& s, int tile) {
   Kv8Tiles t;
-  t.first = tile & ~1;
-  t.count = t.first + 1 < plan.n_tiles ? 2 : 1;
+  t.first = plan.paired ? tile & ~1 : tile;
+  t.count = plan.paired && t.first + 1 < plan.n_tiles ? 2 : 1;
   const int Nv = s.rows * a.G, r_end = min(s.rows, ((t.first + t.count) * 128 - 1) / a.G + 1);   // rows below r_end
   const int fresh = a.k_new == nullptr ? 0 : a.mask != nullptr ? s.rows : r_end;
   t.cached = (s.len + 127) >> 7;
   t.steps = t.first * 128 < Nv ? t.cached + ((fresh + 127) >> 7) : 0;
-  t.split = kv8_split(t.steps, t.count == 2 ? plan.chunk : 2 * plan.chunk, 1);
+  t.split = kv8_split(t.steps, plan.paired && t.count == 1 ? 2 * plan.chunk : plan.chunk, 1);
   return t;
 }
 

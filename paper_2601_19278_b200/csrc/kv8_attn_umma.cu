@@ -212,10 +212,10 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
   const int h = blockIdx.x, b = blockIdx.y;
   const Kv8Seq s = kv8_seq(a, b, tid == 0 && h == 0 && blockIdx.z == 0);
   // unit -> (group of row tiles, chunk): chunk-major, so that the full chunks of all sequences start first
-  const int groups = (plan.n_tiles + 1) / 2;
+  const int groups = plan.paired ? (plan.n_tiles + 1) / 2 : plan.n_tiles;
   // (and the heavier groups: of a chunk the last rows, which see most; else the pairs before a single tile)
   const int nth = (int)blockIdx.z % groups, group = CHUNK ? groups - 1 - nth : nth, chunk_id = (int)blockIdx.z / groups;
-  const Kv8Tiles tl = kv8_tiles(a, plan, s, 2 * group);
+  const Kv8Tiles tl = kv8_tiles(a, plan, s, plan.paired ? 2 * group : group);
   pdl_trigger();                   // the join may be scheduled as SMs drain; it waits for this grid
   if (chunk_id >= tl.split.n) return;
   const int j0 = chunk_id * tl.split.per, n = min(tl.steps - j0, tl.split.per);     // this CTA's steps j0 .. j0 + n - 1
@@ -776,23 +776,35 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
 // six steps, and a partial result is written, read again and joined, so the keys are split only as far as one wave of
 // CTAs, one to an SM, goes.  (Measured, steps per CTA: 16 ragged sequences of up to 65 steps, 256 cells: 65 steps 169 us, 33: 192,
 // 16: 226; prompt chunk, 256 cells of 44: 44 steps 291 us, 22: 353; one tree, 16 cells of 33 steps: 4 steps 32 us, 3: 37, 8: 38.)
+// A step of two row tiles takes about 2.2 us and the CTA around it 15; a step of one tile 1.6 us and its CTA 11: two tiles
+// are cheaper by the row, one tile is done sooner where the GPU is not full anyway (one tree, 3 tiles of 8 heads: @ONE).
 void kv8_umma_plan(const Kv8AttnArgs& a, Kv8Plan& p) {
   constexpr int kSms = 148, kMinSteps = 4;
   p.n_tiles = (a.rows * a.G + 127) / 128;
-  const long long groups = (p.n_tiles + 1) / 2, cells = groups * a.batch * a.c.hkv;
+  const long long heads = (long long)a.batch * a.c.hkv;
   const int steps = (int)(((long long)a.max_len + 127) / 128) + (a.k_new != nullptr ? (a.rows + 127) / 128 : 0);
   const long long all = ((long long)a.max_len + 127) / 128 + (a.rows + 127) / 128;       // whether or not there are new rows
-  const long long parts = cells >= kSms ? 1 : kSms / cells;
-  long long chunk = (steps + parts - 1) / parts;
-  if (chunk < kMinSteps) chunk = kMinSteps;
-  const long long longest = all * groups / 63487 + 1;                                     // the grid's third dimension
-  if (chunk < longest) chunk = longest;
-  p.chunk = (int)chunk;
+  double best = 0.0;
+  long long most = 0;             // parts that no smaller max_len exceeds, in either form
+  for (int paired = 0; paired < 2; ++paired) {
+    if (paired && p.n_tiles == 1) break;
+    const long long groups = paired ? (p.n_tiles + 1) / 2 : p.n_tiles, cells = groups * heads;
+    const long long parts = cells >= kSms ? 1 : kSms / cells;
+    long long chunk = (steps + parts - 1) / parts;
+    if (chunk < kMinSteps) chunk = kMinSteps;
+    const long long longest = all * groups / 63487 + 1;                                   // the grid's third dimension
+    if (chunk < longest) chunk = longest;
+    const double waves = cells >= kSms ? (double)cells / kSms : 1.0, cost = waves * (paired ? 15.0 + 2.2 * chunk : 11.0 + 1.6 * chunk);
+    if (paired == 0 || cost < best) {
+      best = cost;
+      p.paired = paired;
+      p.chunk = (int)chunk;
+    }
+    if (parts > most) most = parts;
+  }
   p.max_chunks = kv8_split(steps, p.chunk, 1).n;
-  // no shorter max_len needs more parts than this
-  long long most = (all + kMinSteps - 1) / kMinSteps;
-  if (most > parts) most = parts;
-  p.bytes = most > 1 ? (size_t)a.batch * a.c.hkv * p.n_tiles * 128 * (size_t)most : 0;
+  if (most > (all + kMinSteps - 1) / kMinSteps) most = (all + kMinSteps - 1) / kMinSteps;
+  p.bytes = most > 1 ? (size_t)heads * p.n_tiles * 128 * (size_t)most : 0;                // partial rows
 }
 
 namespace {
@@ -801,7 +813,7 @@ cudaError_t launch_kernel(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStream_t s
   const auto kernel = kv8_attn_umma_kernel<FMT, DH, CHUNK>;
   const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), KuLayout<DH>::smem);
   if (e != cudaSuccess) return e;
-  kernel<<<dim3(a.c.hkv, a.batch, (p.n_tiles + 1) / 2 * p.max_chunks), kKuThreads, KuLayout<DH>::smem, st>>>(a, p);
+  kernel<<<dim3(a.c.hkv, a.batch, (p.paired ? (p.n_tiles + 1) / 2 : p.n_tiles) * p.max_chunks), kKuThreads, KuLayout<DH>::smem, st>>>(a, p);
   return cudaGetLastError();
 }
 template <int FMT, int DH>
