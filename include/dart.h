@@ -407,7 +407,8 @@ typedef struct dart_kv8_cache {
   int32_t head_dim;      /* 64 or 128 */
   void* k_pages;         /* DEVICE u8  [n_layers, n_pages, n_kv_heads, page_tokens, head_dim], 16-byte aligned */
   void* v_pages;         /* DEVICE u8, same layout */
-  float* k_scale;        /* DEVICE f32 [n_layers, n_pages, n_kv_heads]; positive and finite for pages in use */
+  float* k_scale;        /* DEVICE f32 [n_layers, n_pages, n_kv_heads]; for pages in use 2^-100 .. 2^120 (the append writes
+                            powers of two from 2^-64 on) */
   float* v_scale;        /* DEVICE f32, same layout */
 } dart_kv8_cache;
 
@@ -417,7 +418,9 @@ typedef struct dart_kv8_cache {
  * mask[b][r][y] != 0 (a draft tree's attention mask as dart_build_tree writes it, self included); new rows from
  * n_rows[b] on do not exist.  Without k_new / v_new the rows read the cache alone.  Grouped-query heads: head j reads KV
  * head j / (n_q_heads / n_kv_heads).  Softmax scale 1 / sqrt(head_dim), keys post-RoPE.  Every row of `out` is written;
- * rows that see no key and rows from n_rows[b] on are zero.  What hidden rows, rows that do not exist and positions
+ * rows that see no key and rows from n_rows[b] on are zero.  Sums are fp32; weights enter the second product as fp16 (2^-11
+ * relative), relative to what a key contributes (weight times value scale), so the scales of a sequence may lie far apart
+ * (a span of 2^90 is safe).  What hidden rows, rows that do not exist and positions
  * behind a sequence's length hold (infinities and NaN included) does not reach the output.
  */
 typedef struct dart_kv8_attn_in {

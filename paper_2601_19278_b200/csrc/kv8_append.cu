@@ -37,13 +37,15 @@ __device__ __forceinline__ float kv8_value(uint32_t code) {
 }
 
 // One team of threads per (layer, batch entry, touched page, KV head, K or V): a warp where a call adds at most 16 rows of
-// 128 to a page (a decoding step, an accepted path), else a block of 256.  What bounds both is latency, not bytes: length
+// 128 to a page (a decoding step, an accepted path), else a block of 128.  What bounds both is latency, not bytes: length
 // -> rows and page id -> scale -> codes is a chain of three dependent reads of about a microsecond each, so the rows of
 // a unit are all requested at once, before the page is known, and stay in registers between the maximum and the rounding,
-// and the units in flight have to fill the GPU: eight per block of warp teams, and no more registers than the page size
-// asks for in a block team (PIECES 16-byte pieces per thread).
-// Measured: 16 x 9 rows x 16 layers x 8 heads 39.0 -> @ACC us with warp teams; 4 x 2047 rows x 8 heads 35.4 -> @PRO us with
-// the reads ahead of the page and registers by page size.
+// and the units in flight have to fill the GPU: four per block of warp teams, and no more registers than the page size
+// asks for in a block team (PIECES 16-byte pieces per thread).  Next to the latencies it is instructions: a page's
+// largest value comes from 16-bit three-way maxima of the raw words, rows are found by adding a stride.
+// Measured: 16 accepted paths x 16 layers x 8 heads (8.3 MB) 7.1 us, 39 with a block of 256 per unit; 4 x 2047 prompt rows x
+// 8 heads (50 MB) 13.4 us = 0.57 of the copy peak, 35 with the rows read after the page, 20 with element-wise maxima, 14.9
+// in blocks of 256, 19 in warp teams; strips of pages per block, the next page's rows in flight: 32.
 constexpr int kApThreads = 128;
 
 template <int TEAM>

@@ -23,7 +23,7 @@ namespace dart {
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------
 // What bounds it is the stream of K and V bytes, and that takes bytes in flight: about 60 KB per SM, which registers cannot
-// hold beside the accumulators (with one group of 16 keys ahead in registers, 48 KB per SM: 5.0 TB/s; @STREAM).  Every warp
+// hold beside the accumulators (with one group of 16 keys ahead in registers, 48 KB per SM, 64 ragged sequences took 126 us; from the rings 96 us = 5.9 TB/s, 0.91 of the copy peak).  Every warp
 // therefore has a ring of its own in shared memory, kStStages groups of 16 keys deep, filled by 16-byte asynchronous
 // copies; rows are laid out so that the reads below meet no bank twice.  From there every lane reads exactly the bytes that
 // its own tensor-core fragments need:
@@ -436,7 +436,8 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
 
 // ---- the join ---------------------------------------------------------------------------------------------------------
 // WPR warps per row, partials in a fixed order.  Sequences that fit one chunk were finished by their only CTA.  What bounds
-// it is one row's chain of reads: with 54 partials a single warp took 38 us, eight warps take @CMB.
+// it is one row's chain of reads, so eight partials are read at a time: with 54 partials a single warp and two dependent rounds
+// took 38 us, eight warps and one round take about 4.
 template <int WPR>
 __global__ void __launch_bounds__(256) kv8_combine_kernel(const __grid_constant__ Kv8AttnArgs a, const Kv8Plan plan) {
   constexpr int kRows = 8 / WPR;
@@ -464,18 +465,32 @@ __global__ void __launch_bounds__(256) kv8_combine_kernel(const __grid_constant_
   float M = -INFINITY, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   if (n > 1) {
-    for (int c = w + lane * WPR; c < n; c += 32 * WPR) M = fmaxf(M, plan.ml_part[(part0 + c * step) * 2]);
-    M = warp_max(M);
     const int c4 = min(lane, dh / 4 - 1);
-#pragma unroll 4
-    for (int c = w; c < n; c += WPR) {
-      const size_t p = part0 + c * step;
-      const float2 ml = *reinterpret_cast<const float2*>(plan.ml_part + p * 2);
-      const float4 v = *reinterpret_cast<const float4*>(plan.o_part + p * dh + c4 * 4);
-      if (ml.y == 0.f) continue;      // no key in this chunk
-      const float f = exp2f(ml.x - M);
-      L += ml.y * f;
-      acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+#pragma unroll 1
+    for (int c0 = w; c0 < n; c0 += 8 * WPR) {      // eight partials at a time, all their reads in flight together
+      float2 ml[8];
+      float4 v[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const size_t p = part0 + min(c0 + q * WPR, n - 1) * step;
+        ml[q] = *reinterpret_cast<const float2*>(plan.ml_part + p * 2);
+        v[q] = *reinterpret_cast<const float4*>(plan.o_part + p * dh + c4 * 4);
+      }
+      float mn = M;
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (c0 + q * WPR < n) mn = fmaxf(mn, ml[q].x);
+      const float up = M == mn ? 1.f : exp2f(M - mn);      // 0 the first time
+      M = mn;
+      L *= up;
+      acc.x *= up; acc.y *= up; acc.z *= up; acc.w *= up;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        if (c0 + q * WPR >= n || ml[q].y == 0.f) continue;      // no key in this chunk
+        const float f = exp2f(ml[q].x - M);
+        L += ml[q].y * f;
+        acc.x += v[q].x * f; acc.y += v[q].y * f; acc.z += v[q].z * f; acc.w += v[q].w * f;
+      }
     }
   }
   if (WPR > 1) {

@@ -5,16 +5,24 @@
 //   * two row tiles: both pipelines use every key step, so a step's codes are fetched and converted once for 256 rows;
 //   * one row tile (up to 128 rows, or an odd last tile): the key steps alternate between the pipelines, whose results are
 //     joined at the end.
-// Data path of a step: the producer warp copies the codes of 64 keys at a time (a page, several, or half of one:
-// cp.async.bulk, the pages lie where the table says) into a ring of shared-memory slots; four converter warps turn
-// them into fp16 (exact) K and V tiles in the 128-byte-swizzle operand layout, two buffers each, and write every key's
-// scales beside them; an issuer thread per pipeline runs
-//   S = Q K^T   tcgen05.mma 128 x 128, k = DH, Q and K from shared memory, S fp32 in tensor memory
-//   O += P V    tcgen05.mma 128 x DH, k = 64 twice, P (fp16) from TENSOR memory, V as stored ([keys][DH], MN-major B)
-// and four softmax warps per pipeline (a row per thread) read S 64 columns at a time, and write P over the columns of S
-// they have already read.  P in tensor memory instead of shared memory: the MMAs are bound by shared-memory operand reads
-// here (128 x 128 x 16 reads 8 KB = 64 cycles' worth from two shared operands, 4 KB with one in tensor memory), and the
-// room is needed for the converted tiles.
+// Data path of a step: two producer warps copy the codes of 64 keys at a time (a page, several, or half of one:
+// cp.async.bulk, the pages lie where the table says) into rings of shared-memory slots, K and V apart; four converter
+// warps for each turn them into fp16 (exact) tiles in the 128-byte-swizzle operand layout, two buffers each, and write
+// every key's scales; an issuer warp per pipeline runs, in half steps of 64 keys,
+//   S = Q K^T   tcgen05.mma 128 x 64, k = DH, Q and K from shared memory, S fp32 in tensor memory, two buffers
+//   O += P V    tcgen05.mma 128 x DH, k = 64, P (fp16) from TENSOR memory, V as stored ([keys][DH], MN-major B)
+// and four softmax warps per pipeline (a row per thread) read the scores of a half step and write P over them.  P in tensor
+// memory instead of shared memory: operand reads from shared memory are what is scarce, and the room is needed for the
+// converted tiles.
+// What bounds a step of 256 rows x 128 keys (2.2 us = 1.1 PFLOP/s in all, 0.7 of the bf16 peak): the exponentials (two softmax
+// warps share a special-function unit: 1.1 us) and shared memory (operands, codes and converted tiles: about 1.5 us of
+// its bandwidth), neither alone: without the exponentials a step takes 1.8, without half of the MMAs 2.1.  What was tried:
+// part of the exponentials as polynomials (no faster with two warps to a unit), scores in steps of 128 keys without a second
+// buffer (the chain S -> P -> O showed: 2.5), one producer for K and V and half the converters (2.3 to 3.9 while they
+// were the slowest role), exponentials interleaved with their sums instead of in phases (3 %).
+// A CTA's start and end cost 9 to 13 us (queries to fp16 4, the first scores 3, the result 2) and new rows that only some
+// rows see 5 us a step, which is most of a short call.  Code outside the inner loops is kept in loops and short:
+// unrolled, it was 100 KB and each CTA waited for its instructions.
 // New rows are read by the converters themselves, each key divided by its own power of two; a value that is not finite is
 // kept out of the product (0 weight times NaN would reach rows that do not see it) and added at the end to the rows that do.
 // Every wait is bounded.
@@ -30,12 +38,13 @@ constexpr int kKuThreads = 640;      // warps 0: producer of K, 1 and 3: MMA iss
 constexpr int kKuPairSlots = 2, kKuSingleSlots = 3;     // 64-key code slots of each ring (K, V): what shared memory leaves
 constexpr int kKuBad = 4096 / 32;
 
-// Bounded wait in little code (the loop is not unrolled: there are some twenty of them).  try_wait may suspend the warp,
-// which leaves the issue slots to the softmax warps beside it (1 % of the kernel's time against test_wait, with or without a
-// pause between two looks).  After some seconds the CTA's abort flag is raised and all roles leave.
+// Bounded wait in little code (the loop is not unrolled: there are some twenty of them).  try_wait suspends the warp for up to
+// 2600 cycles (measured), which leaves the issue slots to the softmax warps beside it (1 % of the kernel's time against
+// test_wait, with or without a pause between two looks; with a suspend-time hint, or a look at the clock, 2 to 3 % slower).
+// A million tries, about a second and a half, then the CTA's abort flag is raised and all roles leave.
 __device__ __forceinline__ bool ku_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
 #pragma unroll 1
-  for (int it = 0; it < 4000000; ++it) {
+  for (int it = 0; it < 1000000; ++it) {
     uint32_t ok;
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                  : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
@@ -775,9 +784,10 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
 // Key steps of a CTA.  A CTA's start and end (queries, the first copies, the first scores, its result) cost as much as five or
 // six steps, and a partial result is written, read again and joined, so the keys are split only as far as one wave of
 // CTAs, one to an SM, goes.  (Measured, steps per CTA: 16 ragged sequences of up to 65 steps, 256 cells: 65 steps 169 us, 33: 192,
-// 16: 226; prompt chunk, 256 cells of 44: 44 steps 291 us, 22: 353; one tree, 16 cells of 33 steps: 4 steps 32 us, 3: 37, 8: 38.)
+// 16: 226; prompt chunk, 256 cells of 44: 44 steps 291 us, 22: 353; one tree in pairs, 16 cells of 33 steps: 4 steps 32 us, 3: 37, 8: 38.)
 // A step of two row tiles takes about 2.2 us and the CTA around it 15; a step of one tile 1.6 us and its CTA 11: two tiles
-// are cheaper by the row, one tile is done sooner where the GPU is not full anyway (one tree, 3 tiles of 8 heads: @ONE).
+// are cheaper by the row, one tile is done sooner where the GPU is not full anyway (one tree over 33 steps,
+// 3 tiles of 8 heads: 28.4 us in single tiles, 31.9 in pairs).
 void kv8_umma_plan(const Kv8AttnArgs& a, Kv8Plan& p) {
   constexpr int kSms = 148, kMinSteps = 4;
   p.n_tiles = (a.rows * a.G + 127) / 128;

@@ -7,6 +7,9 @@ product rounded to fp16 (2^-11 each) or are kept in fp32; a score off by e chang
 2^-25 of the row's largest element): e <= 2^-19 * sum |q_i k_i| / sqrt(d).  With A = sum p |v|: error <= 2^-8 |ref| +
 (2^-10 + 2^-18 X) A, plus 2^-20 of the largest |v| for elements that fp16 cuts off."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -282,6 +285,56 @@ def test_prompt_chunks_whose_new_rows_dominate(R, H, hkv, big):
     vn *= torch.exp2(torch.randint(-6, 7, (1, R, 1, 1)).float())
     got = attend(c, 0, q.to(DEV), kn.to(DEV), vn.to(DEV), 140)
     check(c, 0, got, q, kn, vn, only=[0, 1, 63, 64, 127, 128, 129, 191, 192, 255, 256, 257, R - 1])
+
+
+@pytest.mark.parametrize("B,R,H,hkv,d,lens", [(3, 1, 128, 1, 128, [70, 0, 300]), (2, 1, 256, 2, 64, [33, 500]), (1, 4096, 1, 1, 64, [100]),
+                                              (1024, 1, 4, 2, 64, [i % 37 for i in range(1024)]), (2, 1, 256, 256, 64, [20, 40])])
+def test_the_largest_shapes(B, R, H, hkv, d, lens):
+    c = Case(lens, 16, "e4m3", hkv, d, seed=B + R)
+    q, kn, vn = c.bf16(B, R, H, d), c.bf16(B, R, hkv, d), c.bf16(B, R, hkv, d)
+    got = attend(c, 0, q.to(DEV), kn.to(DEV), vn.to(DEV), max(lens))
+    check(c, 0, got, q, kn, vn, only=[0, 1, 127, 128, R // 2 + 3, R - 1] if R > 1 else None)
+
+
+def test_a_first_call_may_be_captured():
+    """A process whose first attention calls (both kernels) lie inside a graph capture."""
+    code = """
+import sys; sys.path.insert(0, {root!r})
+import torch
+from paper_2601_19278_b200 import binding as b
+dev = "cuda:0"
+k, v = (torch.randint(-99, 99, (1, 9, 2, 16, 64), device=dev).to(torch.int8) for _ in range(2))
+s = torch.full((1, 9, 2), 2.0 ** -6, device=dev)
+c = b.Kv8Cache(k, v, s, s.clone())
+table, lens = torch.arange(8, dtype=torch.int32, device=dev).view(1, 8), torch.tensor([100], dtype=torch.int32, device=dev)
+calls = []
+for R in (1, 20, 200):
+    q, kn, vn = (torch.randn(1, R, h, 64, device=dev).bfloat16() for h in (4, 2, 2))
+    out, ws = torch.zeros_like(q), torch.empty(b.kv8_attention_workspace_bytes(c, 1, R, 4, 128), dtype=torch.uint8, device=dev)
+    calls.append((q, kn, vn, out, ws))
+run = lambda outs: [b.kv8_attention(c, 0, q, kn, vn, lens, table, o, max_len=128, workspace=ws) for (q, kn, vn, _, ws), o in zip(calls, outs)]
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    run([x[3] for x in calls])
+g.replay()
+eager = [torch.zeros_like(x[3]) for x in calls]
+run(eager)
+torch.cuda.synchronize()
+assert all(torch.equal(a, x[3]) and bool(a.any()) for a, x in zip(eager, calls))
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code.format(root=root)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0, r.stdout[-2000:]
+
+
+def test_append_takes_the_first_rows_without_counts():
+    c = Case([3, 0], 16, "int8", 1, 64, seed=41, room=8)
+    kn, vn = c.bf16(1, 2, 5, 1, 64), c.bf16(1, 2, 5, 1, 64)
+    b.kv8_append(c.cache, 0, kn.to(DEV), vn.to(DEV), c.seq_lens, c.table, max_append=2)
+    for i in range(2):
+        c.pool.append(0, c.pages[i], c.lens[i], kn[0, i, :2].double().numpy(), vn[0, i, :2].double().numpy())
+    same_pool(c)
 
 
 def test_pools_past_four_gigabytes():
