@@ -20,7 +20,8 @@ constexpr int kPgThreads = 1024;
 constexpr int kPgHead = 16;
 size_t kv8_pages_workspace(int n_pages) { return ((size_t)kPgHead + 4 * (size_t)n_pages) * sizeof(int); }
 
-// Exclusive prefix sum of v over the block's threads; *total gets the sum.  sh: 33 ints; the caller syncs before reuse.
+// Exclusive prefix sum of v <= 2^24 + 1 over the block's threads; *total gets the sum.  sh: 33 ints; the caller syncs before
+// reuse.  A warp's sum counts as 2^25 at most, so that nothing overflows: sums above 2^24 are above it, no more.
 __device__ __forceinline__ int block_scan(int v, int* sh, int* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int x = v;
@@ -30,7 +31,7 @@ __device__ __forceinline__ int block_scan(int v, int* sh, int* total) {
     if (lane >= o) x += y;
   }
   __syncthreads();
-  if (lane == 31) sh[warp] = x;
+  if (lane == 31) sh[warp] = min(x, 1 << 25);
   __syncthreads();
   if (warp == 0) {
     const int s = lane < (int)(blockDim.x >> 5) ? sh[lane] : 0;
@@ -132,7 +133,10 @@ __global__ void __launch_bounds__(kPgThreads) kv8_reserve_plan_kernel(const Kv8P
   }
   s_lo[tid] = lo;
   int total_cols, total_need = 0;
-  const int start = block_scan(width, sh, &total_cols);
+  const int start = block_scan(min(width, p.n_pages + 1), sh, &total_cols);
+  // every listed column ends up with a page of its own: more columns than pages cannot be had
+  const bool too_many = total_cols > p.n_pages;
+  if (too_many) total_cols = 0;
   s_start[tid] = start;
   if (tid == 0) s_start[kPgThreads] = total_cols;
   __syncthreads();
@@ -170,7 +174,7 @@ __global__ void __launch_bounds__(kPgThreads) kv8_reserve_plan_kernel(const Kv8P
     }
     int here;
     const int k = total_need + block_scan(need, sh, &here);
-    if (need && k < p.n_pages) { src[k] = old; slot[k] = s; column[k] = j; }
+    if (need) { src[k] = old; slot[k] = s; column[k] = j; }
     total_need += here;
   }
   __syncthreads();
@@ -194,7 +198,7 @@ __global__ void __launch_bounds__(kPgThreads) kv8_reserve_plan_kernel(const Kv8P
     found += here;
   }
   __syncthreads();
-  const bool ok = found >= total_need;
+  const bool ok = !too_many && found >= total_need;
   if (ok)
     for (int k = tid; k < total_need; k += kPgThreads) {
       const int page = dst[k];

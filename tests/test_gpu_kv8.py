@@ -676,6 +676,24 @@ def test_a_pool_without_enough_pages_changes_nothing():
     s.check()
 
 
+def test_a_reserve_of_more_than_two_to_the_31_columns_changes_nothing():
+    S, M, P = 1024, (1 << 21) + 8, 32
+    i32 = Server.i32
+    table, lens, ref = torch.full((S, M), -1, dtype=torch.int32, device=DEV), i32([0] * S), i32([0] * P)
+    pages = b.Kv8Pages(table, lens, ref, 16)
+    k, v = (torch.zeros(1, P, 1, 16, 64, dtype=torch.int8, device=DEV) for _ in range(2))
+    cache = b.Kv8Cache(k, v, torch.ones(1, P, 1, device=DEV), torch.ones(1, P, 1, device=DEV))
+    ws, status = torch.empty(b.kv8_pages_workspace_bytes(pages), dtype=torch.uint8, device=DEV), i32([0])
+    for n in (M * 16, (1 << 20) * 16):                      # 2^31 + 8192 and 2^30 columns
+        status.zero_()
+        b.kv8_reserve(pages, cache, i32(range(S)), i32([n] * S), workspace=ws, status=status)
+        assert int(status) == b.DART_ERR_CAPACITY
+        assert int(table.max()) == -1 and int(table.min()) == -1 and not ref.any() and not lens.any()
+    status.zero_()
+    b.kv8_reserve(pages, cache, i32(range(S)), i32([16] * P + [0] * (S - P)), workspace=ws, status=status)
+    assert int(status) == 0 and table[:P, 0].tolist() == list(range(P)) and ref.tolist() == [1] * P and int(table[P:].max()) == -1
+
+
 def test_many_sequences_and_pages():
     """More pages than one round of the planning scan, lists longer than a warp, sharers listed and not."""
     s = Server(20000, 16, 700, 40, hkv=1, layers=1, seed=5)
