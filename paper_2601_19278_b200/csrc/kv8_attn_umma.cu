@@ -302,7 +302,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       if (lane == 0) mbar_expect_tx(&full[st], max(live, 0) * bytes);      // 0: the slot lies behind the end, the phase completes
       __syncwarp();
       // two slots are little time for the way from HBM: the lines two steps on are asked into L2
-      const int ahead = col + 4 * (a.c.pt_log2 < 6 ? pages : 1);
+      const int ahead = col + (256 >> a.c.pt_log2);
       const int page4 = __shfl_sync(0xffffffffu, ahead < 32 * (window + 1) ? ids : ids_next, (ahead + lane) & 31);
       if (pair && lane < pages && t + 4 < total) bulk_prefetch(base + page4 * page_bytes + (((t + 4) << 6) & (a.c.pt - 1)) * DH, bytes);
       if (lane < live) bulk_load(ring + st * Ly::slot + lane * bytes, base + page * page_bytes + (key & (a.c.pt - 1)) * DH, bytes, &full[st]);
