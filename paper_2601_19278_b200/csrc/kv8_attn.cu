@@ -11,8 +11,8 @@
 // rounding to fp16 (2^-11, or 2^-25 absolute for weights that do not matter) is relative to what the key contributes,
 // however far apart the pages' scales are.  m, l and O are fp32.  New rows are keys with a power-of-two scale of their own.
 //
-// Rows of all query heads that share a KV head are one matrix (row r, head g of the group -> r * G + g).  Up to 16 such
-// rows run on kv8_attn_stream_kernel below: a stream of the cache at memory speed.  More rows run on tcgen05
+// Rows of all query heads that share a KV head are one matrix (row r, head g of the group -> r * G + g).  Up to 24 such
+// rows (32 with d = 64: kv8_stream_rows) run on kv8_attn_stream_kernel below: a stream of the cache at memory speed.  More rows run on tcgen05
 // (kv8_attn_umma.cu).  A long key axis is split over CTAs; their partial (m, l, O) go through the workspace and
 // kv8_combine_kernel joins them.
 #include <string.h>
@@ -23,10 +23,10 @@ namespace dart {
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------
 // What bounds it is the stream of K and V bytes, and that takes bytes in flight: about 60 KB per SM, which registers cannot
-// hold beside the accumulators (with one group of 16 keys ahead in registers, 48 KB per SM, 64 ragged sequences took 126 us; from the rings 96 us = 5.9 TB/s, 0.91 of the copy peak).  Every warp
-// therefore has a ring of its own in shared memory, kStStages groups of 16 keys deep, filled by 16-byte asynchronous
-// copies; rows are laid out so that the reads below meet no bank twice.  From there every lane reads exactly the bytes that
-// its own tensor-core fragments need:
+// hold beside the accumulators (with one group of 16 keys ahead in registers, 48 KB per SM, 64 ragged sequences took 126 us;
+// from the rings 96 us = 5.9 TB/s, 0.91 of the copy peak).  Every warp therefore has a ring of its own in shared
+// memory, kStStages groups of 16 keys deep, filled by 16-byte asynchronous copies; rows are laid out so that the reads below
+// meet no bank twice.  From there every lane reads exactly the bytes that its own tensor-core fragments need:
 //   S^T = K Q^T    mma m16n8k16 with the 16 keys as M.  The order of the contraction index is free as long as Q and K agree:
 //                  lane t of a key's quad takes d = [t * DH/4, (t+1) * DH/4), whole 16-byte words of the key's row.
 //   O^T = V^T P^T  the same instruction with d as M: its A operand wants pairs of neighbouring keys, which two bytes of
@@ -67,9 +67,17 @@ constexpr __host__ __device__ int st_body() {
   return kStWarps * kStStages * 2 * 16 * DH > kStWarps * 8 * NT * DH * 4 ? kStWarps * kStStages * 2 * 16 * DH : kStWarps * 8 * NT * DH * 4;
 }
 
-// NT tiles of 8 rows: up to 8 or up to 16 rows.
+// NT tiles of 8 rows.  With more of them the instructions per byte grow and registers run out (O and Q take 48 NT a thread at
+// d = 128, 24 NT at 64), which sets how many CTAs fit an SM; tcgen05 converts a step's codes at one cost for 1 to 128 rows.
+// Both sides, 8 KV heads, e4m3, us here and there: 16 sequences of 8192 keys, d = 128: 20 rows 87, 107; 32 rows 148
+// (spilled), 107; d = 64: 24 rows 63, 91; 32 rows 72, 91.  64 of 2048, d = 128: 20 rows 101, 146; d = 64: 32 rows 87, 122.
+// A single sequence of 8192 loses: d = 128, 20 rows 18.4, 17.4; d = 64, 32 rows 16.6, 15.3.
+// d = 64, 64 sequences of 2048 keys: four CTAs to an SM instead of three for 8 rows 37 us, 41; three instead of two for 16 rows
+// 50, 57.
+constexpr __host__ __device__ int kv8_stream_ctas(int dh, int nt) { return nt == 1 ? (dh == 64 ? 4 : 3) : nt == 2 && dh == 64 ? 3 : 2; }
+constexpr __host__ __device__ int kv8_stream_rows(int dh) { return dh == 64 ? 32 : 24; }
 template <int FMT, int DH, int NT>
-__global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_stream_kernel(const __grid_constant__ Kv8AttnArgs a,
+__global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_attn_stream_kernel(const __grid_constant__ Kv8AttnArgs a,
                                                                                         const Kv8Plan plan) {
   constexpr int MT = DH / 16, KW = DH / 16;     // d tiles of the second product; words of a lane's piece of a key
   constexpr int NR = 8 * NT;
@@ -281,8 +289,10 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
     }
   }
 
-  // ---- the new rows (at most 16): one more group, on the last chunk's first warp, each key divided by a power of two
-  if (last && warp == 0 && a.k_new != nullptr && s.rows > 0) {
+  // ---- the new rows, 16 at a time, on the last chunk's first warp, each key divided by a power of two
+  const int fresh = last && warp == 0 && a.k_new != nullptr ? s.rows : 0;
+#pragma unroll 1
+  for (int y0 = 0; y0 < fresh; y0 += 16) {
     const bf16* kn = a.k_new + (size_t)((long long)b * a.rows) * a.new_stride + (size_t)h * DH;
     const bf16* vn = a.v_new + (kn - a.k_new);
     float x[NT][4], ksc[2];                      // scale of keys g, g + 8
@@ -291,10 +301,10 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
     uint4 raw[2][DH / 32];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const bool on = g + 8 * i < s.rows;
+      const bool on = y0 + g + 8 * i < s.rows;
 #pragma unroll
       for (int e = 0; e < DH / 32; ++e)
-        raw[i][e] = on ? *(reinterpret_cast<const uint4*>(kn + (size_t)(g + 8 * i) * a.new_stride + t * (DH / 4)) + e) : make_uint4(0u, 0u, 0u, 0u);
+        raw[i][e] = on ? *(reinterpret_cast<const uint4*>(kn + (size_t)(y0 + g + 8 * i) * a.new_stride + t * (DH / 4)) + e) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -321,7 +331,7 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
     bool odd = false;                            // a value that is not finite
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int y = 2 * t + (e & 1) + 8 * (e >> 1);
+      const int y = y0 + 2 * t + (e & 1) + 8 * (e >> 1);
       const bool on = y < s.rows;
       uint4 rv[DH / 64];
       uint32_t big = 0;
@@ -352,7 +362,7 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = 2 * t + (e & 1) + 8 * n, y = g + 8 * (e >> 1);
+        const int i = 2 * t + (e & 1) + 8 * n, y = y0 + g + 8 * (e >> 1);
         const bool see = i < Nv && y < s.rows && kv8_sees(a, b, i / a.G, y);
         x[n][e] = see ? fmaf(x[n][e], crow[n][e & 1] * ksc[e >> 1], (float)evk[e >> 1]) : -INFINITY;
       }
@@ -372,7 +382,7 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
     }
     if (__any_sync(0xffffffffu, odd)) {          // values that are not finite reach exactly the rows that see them
 #pragma unroll 1
-      for (int y = 0; y < s.rows; ++y)
+      for (int y = y0; y < min(s.rows, y0 + 16); ++y)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -388,6 +398,7 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
               }
           }
     }
+    if (NT <= 2) break;                            // (16 rows at most: no loop)
   }
 
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -427,7 +438,7 @@ __global__ void __launch_bounds__(kStWarps * 32, NT == 1 ? 3 : 2) kv8_attn_strea
     if (sp.n == 1) {
       kv8_store_row(a, b, h, i, i < Nv, L, c4, acc);
     } else {
-      const size_t part = ((size_t)(b * a.c.hkv + h) * plan.max_chunks + chunk_id) * 16 + i;
+      const size_t part = ((size_t)(b * a.c.hkv + h) * plan.max_chunks + chunk_id) * NR + i;
       *reinterpret_cast<float4*>(plan.o_part + part * DH + c4 * 4) = acc;
       if (c4 == 0) *reinterpret_cast<float2*>(plan.ml_part + part * 2) = make_float2(M, L);
     }
@@ -448,16 +459,16 @@ __global__ void __launch_bounds__(256) kv8_combine_kernel(const __grid_constant_
   const Kv8Seq s = kv8_seq(a, b, false);
   const int N = a.rows * a.G, Nv = s.rows * a.G;
   int n = 0;
-  size_t part0 = 0, step = 16;
+  size_t part0 = 0, step = 128;
   if (i < N) {
     if (plan.umma) {
       const int tile = i >> 7;
       n = kv8_tiles(a, plan, s, tile).split.n;
       part0 = ((size_t)((b * a.c.hkv + h) * plan.n_tiles + tile) * plan.max_chunks) * 128 + (i & 127);
-      step = 128;
     } else {
       n = kv8_split_keys(s.len, plan.chunk).n;
-      part0 = ((size_t)(b * a.c.hkv + h) * plan.max_chunks) * 16 + i;
+      step = (N + 7) / 8 * 8;
+      part0 = ((size_t)(b * a.c.hkv + h) * plan.max_chunks) * step + i;
     }
   }
   pdl_wait();
@@ -518,20 +529,21 @@ __global__ void __launch_bounds__(256) kv8_combine_kernel(const __grid_constant_
 // ---- planning ---------------------------------------------------------------------------------------------------------
 namespace {
 
-// Keys a CTA of the streaming kernel takes.  With few (batch entry, KV head) pairs one wave of CTAs (three to an SM, two with more than 8 rows)
-// shares the longest sequence evenly; with many, whose lengths differ in a way only the device knows, two waves of shorter
-// parts even them out (64 ragged sequences: one wave 98.1 us, two 99.8, four 101.7, six 106.7).  At least 512 keys, so that a CTA's start (page ids, queries, the join) stays a small part.
+// Keys a CTA of the streaming kernel takes.  With few (batch entry, KV head) pairs one wave of CTAs shares the
+// longest sequence evenly; with many, whose lengths differ in a way only the device knows, two waves of shorter parts even
+// them out (64 ragged sequences: one wave 98.1 us, two 99.8, four 101.7, six 106.7).  At least 512 keys, so that a CTA's
+// start (page ids, queries, the join) stays a small part.
 constexpr int kStMinChunk = 512, kStMaxChunk = 8192;
 int round128(long long x) { return (int)((x + 127) / 128 * 128); }
 
 Kv8Plan make_plan(const Kv8AttnArgs& a, void* workspace) {
   Kv8Plan p;
   memset(&p, 0, sizeof(p));
-  p.umma = a.rows * a.G > 16 ? 1 : 0;
+  p.umma = a.rows * a.G > kv8_stream_rows(a.c.dh) ? 1 : 0;
   size_t rows, most;                 // partial rows of this call; of any call with a smaller max_len
   if (!p.umma) {
-    const long long pairs = (long long)a.batch * a.c.hkv;
-    const long long slots = 148 * (a.rows * a.G <= 8 ? 3 : 2), units = pairs * 4 <= slots ? slots : 2 * slots;
+    const long long pairs = (long long)a.batch * a.c.hkv, part = (a.rows * a.G + 7) / 8 * 8;      // rows of a partial result
+    const long long slots = 148 * kv8_stream_ctas(a.c.dh, (a.rows * a.G + 7) / 8), units = pairs * 4 <= slots ? slots : 2 * slots;
     const int parts = (int)((units + pairs - 1) / pairs);               // CTAs per pair if every sequence were the longest
     const int longest = round128(((long long)a.max_len + 65534) / 65535);   // the grid's third dimension
     int chunk = round128(((long long)a.max_len + parts - 1) / parts);
@@ -541,8 +553,8 @@ Kv8Plan make_plan(const Kv8AttnArgs& a, void* workspace) {
     p.n_tiles = 1;
     const long long by_min = ((long long)a.max_len + kStMinChunk - 1) / kStMinChunk, by_max = ((long long)a.max_len + kStMaxChunk - 1) / kStMaxChunk;
     const long long bound = parts > by_max ? parts : by_max;
-    most = (size_t)pairs * 16 * (size_t)(by_min < bound ? by_min : bound);
-    rows = (size_t)pairs * 16 * p.max_chunks;
+    most = (size_t)pairs * part * (size_t)(by_min < bound ? by_min : bound);
+    rows = (size_t)pairs * part * p.max_chunks;
     if (a.max_len <= kStMinChunk) most = 0;
   } else {
     kv8_umma_plan(a, p);
@@ -568,7 +580,10 @@ cudaError_t launch_stream(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStream_t s
 }
 template <int FMT, int DH>
 cudaError_t launch_stream_rows(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStream_t st) {
-  return a.rows * a.G <= 8 ? launch_stream<FMT, DH, 1>(a, p, st) : launch_stream<FMT, DH, 2>(a, p, st);
+  const int n = (a.rows * a.G + 7) / 8;
+  if constexpr (kv8_stream_rows(DH) > 24)
+    if (n == 4) return launch_stream<FMT, DH, 4>(a, p, st);
+  return n == 1 ? launch_stream<FMT, DH, 1>(a, p, st) : n == 2 ? launch_stream<FMT, DH, 2>(a, p, st) : launch_stream<FMT, DH, 3>(a, p, st);
 }
 
 }  // namespace

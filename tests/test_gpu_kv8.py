@@ -296,6 +296,34 @@ def test_the_largest_shapes(B, R, H, hkv, d, lens):
     check(c, 0, got, q, kn, vn, only=[0, 1, 127, 128, R // 2 + 3, R - 1] if R > 1 else None)
 
 
+@pytest.mark.parametrize("R,H,hkv,d,fmt", [(17, 1, 1, 128, "e4m3"), (24, 1, 1, 128, "int8"), (20, 2, 2, 128, "e4m3"), (4, 5, 1, 128, "e4m3"),
+                                           (3, 8, 1, 128, "int8"), (2, 24, 2, 64, "e4m3"), (6, 4, 1, 64, "int8"), (8, 4, 1, 64, "e4m3"),
+                                           (17, 1, 1, 64, "int8"), (32, 1, 1, 64, "e4m3"), (31, 2, 2, 64, "int8"), (25, 1, 1, 128, "e4m3"),
+                                           (33, 1, 1, 64, "int8")])
+def test_seventeen_to_thirty_two_rows(R, H, hkv, d, fmt):
+    """More new rows than one group of 16, three and four tiles of 8 rows, and the first sizes beyond them."""
+    c = Case([301, 0, 16, 33, 5003], 16, fmt, hkv, d, seed=R + H + d)
+    q, kn, vn = c.bf16(5, R, H, d), c.bf16(5, R, hkv, d, scale=2.0), c.bf16(5, R, hkv, d)
+    n_rows = [R, R, max(1, R - 3), min(R, 16), R]
+    dn = torch.tensor(n_rows, dtype=torch.int32, device=DEV)
+    got = attend(c, 0, q.to(DEV), kn.to(DEV), vn.to(DEV), 5003, n_rows=dn)
+    check(c, 0, got, q, kn, vn, n_rows=n_rows)
+    mask = np.stack([tree_mask(c.rng, R, u) for u in n_rows])
+    mask[1, R - 1] = 0                                      # an empty row
+    want = attend(c, 0, q.to(DEV), kn.to(DEV), vn.to(DEV), 5003, n_rows=dn, mask=torch.from_numpy(mask).to(DEV))
+    check(c, 0, want, q, kn, vn, n_rows=n_rows, mask=mask)
+    assert bool((want[1, R - 1] == 0).all())
+    bad_k, bad_v = kn.clone(), vn.clone()                   # what does not exist or is not seen may hold anything
+    for t in (bad_k, bad_v):
+        for x, n in enumerate(n_rows):
+            t[x, n:] = float("nan")
+        t[1, R - 1] = float("inf")
+    mask[1, R - 1, :] = 0
+    mask[1, :, R - 1] = 0
+    got = attend(c, 0, q.to(DEV), bad_k.to(DEV), bad_v.to(DEV), 5003, n_rows=dn, mask=torch.from_numpy(mask).to(DEV))
+    torch.testing.assert_close(got, want, rtol=0, atol=0)
+
+
 def test_a_first_call_may_be_captured():
     """A process whose first attention calls (both kernels) lie inside a graph capture."""
     code = """
