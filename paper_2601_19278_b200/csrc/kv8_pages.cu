@@ -8,7 +8,7 @@
 // cost is their launches and chains of dependent reads, so every kernel here is launched ahead of its predecessor's end
 // (pdl_wait) and the planning kernels compare lists in shared memory.  Measured, with the restoring of the
 // tables between two passes (2 us): 16 sequences forked three times, then all 64 reserved, 40.9 us; one fork and reserve of a
-// short sequence 8.9 us; compaction after releasing half of 64 sequences (169 pages of 16 layers, 709 MB) 137 us, the
+// short sequence 9.8 us; compaction after releasing half of 64 sequences (169 pages of 16 layers, 709 MB) 137 us, the
 // copies alone 122 = 0.89 of the copy peak.
 #include "kv8.cuh"
 
