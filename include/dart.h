@@ -418,9 +418,11 @@ typedef struct dart_kv8_cache {
  * mask[b][r][y] != 0 (a draft tree's attention mask as dart_build_tree writes it, self included); new rows from
  * n_rows[b] on do not exist.  Without k_new / v_new the rows read the cache alone.  Grouped-query heads: head j reads KV
  * head j / (n_q_heads / n_kv_heads).  Softmax scale 1 / sqrt(head_dim), keys post-RoPE.  Every row of `out` is written;
- * rows that see no key and rows from n_rows[b] on are zero.  Sums are fp32; weights enter the second product as fp16 (2^-11
- * relative), relative to what a key contributes (weight times value scale), so the scales of a sequence may lie far apart
- * (a span of 2^90 is safe).  What hidden rows, rows that do not exist and positions
+ * rows that see no key and rows from n_rows[b] on are zero.  Sums are fp32; weights enter the second product as fp16, relative to
+ * what a key contributes (weight times value scale), so the scales of a sequence may lie far apart (a span of 2^90 is safe):
+ * each is off by at most 2^-11 of itself or 2^-34 of the largest, whichever is more.  Queries and new rows enter the products
+ * as fp16 multiples of a power of two near the row's largest element: elements below 2^-17 of it are off by up to 2^-25 of it.
+ * What hidden rows, rows that do not exist and positions
  * behind a sequence's length hold (infinities and NaN included) does not reach the output.
  */
 typedef struct dart_kv8_attn_in {

@@ -131,6 +131,15 @@ __device__ __forceinline__ bool kv8_sees(const Kv8AttnArgs& a, int b, int r, int
   return a.mask != nullptr ? a.mask[((size_t)b * a.rows + r) * a.rows + y] != 0 : y <= r;
 }
 
+// Where a softmax's weights lie in fp16.  A weight that sets the reference maximum is 2^kKv8Bias, and the maximum moves when
+// a key exceeds it by 2^kKv8Rise: 2^15 is the largest weight, which leaves the small ones 2^-25 / 2^9 = 2^-34 of the
+// largest as their rounding.  That has to be small: the largest may belong to a key whose value is next to nothing, and then
+// thousands of small ones make the result.  (With the largest at 1, 8192 keys behind one whose weight is 2^25 times
+// theirs came out as nothing.)  O carries the bias as a factor, m and l do not.  The more bias, the smaller the rise and the
+// more often a row is rescaled: 16 trees of 60 rows over pages whose scales differ by 4 take 172 us with 9, 176 with 11.
+constexpr int kKv8Bias = 9, kKv8Rise = 15 - kKv8Bias;
+constexpr float kKv8Unbias = 1.f / (1 << kKv8Bias);
+
 __device__ __forceinline__ float kv8_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -3,13 +3,15 @@
 //   out[r] = sum_y softmax_y(q[r] . k[y] / sqrt(d)) v[y],   k[y] = s_k * code,  v[y] = s_v * code
 //
 // Codes of both formats are exact in fp16, and so is a bf16 query or new row once divided by a power of two near its
-// largest element, so both products run on fp16 tensor-core instructions with nothing rounded but the weights.  The scales
+// largest element, but for elements below 2^-17 of that (off by up to 2^-25 of it): both products run on fp16 tensor-core
+// instructions with next to nothing rounded but the weights.  The scales
 // never touch the codes: with c = log2(e) / sqrt(d) times the query's power of two, a key of a page with scales s_k, s_v
 // enters as
-//   x = (c s_k) (q . code) + log2(s_v),     P = 2^(x - m),     l += P / s_v,     O += P code,     out = O / l
-// where m follows the largest x (not the largest score): P is the key's weight times its value's scale, at most 2^8, so its
-// rounding to fp16 (2^-11, or 2^-25 absolute for weights that do not matter) is relative to what the key contributes,
-// however far apart the pages' scales are.  m, l and O are fp32.  New rows are keys with a power-of-two scale of their own.
+//   x = (c s_k) (q . code) + log2(s_v),     P = 2^(x - m + 9),     2^9 l += P / s_v,     O += P code,     out = O / (2^9 l)
+// where m follows the largest x (not the largest score): P is the key's weight times its value's scale, 2^15 at most, so its
+// rounding to fp16 is 2^-11 of what the key contributes, however far apart the pages' scales are, or, for P below 2^-14, 2^-34 of
+// the largest weight times scale (kv8.cuh: kKv8Bias); over n keys that is at most n 2^-34 of the largest |v| on the
+// scale of the heaviest key's page.  m, l and O are fp32.  New rows are keys with a power-of-two scale of their own.
 //
 // Rows of all query heads that share a KV head are one matrix (row r, head g of the group -> r * G + g).  Up to 24 such
 // rows (32 with d = 64: kv8_stream_rows) run on kv8_attn_stream_kernel below: a stream of the cache at memory speed.  More rows run on tcgen05
@@ -32,7 +34,7 @@ namespace dart {
 //   O^T = V^T P^T  the same instruction with d as M: its A operand wants pairs of neighbouring keys, which two bytes of
 //                  two keys' words give by one byte permutation before the conversion; P^T is the first product's result
 //                  transposed in 8 x 8 blocks (movmatrix).  Both products give a lane the same two rows, so m and l are its own.
-// m moves only when a score exceeds it by 2^8: the common case has no shuffles at all.  Instructions count next to the bytes
+// m moves only when a score exceeds it by 2^6: the common case has no shuffles at all.  Instructions count next to the bytes
 // (with rows as M in the first product, half of M empty, and scales and addresses from global memory a group of 4 KB took 319
 // of them and the batch of 64 tokens 120 us): scales, their logarithms and the page ids of the CTA's groups are laid out in
 // shared memory once.
@@ -85,7 +87,7 @@ __global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_at
   constexpr int kTile = 16 * DH;                                 // codes of 16 keys
   unsigned char* ring = st_smem + (threadIdx.x >> 5) * (kStStages * 2 * kTile);                       // this warp's
   float(*s_o)[NR][DH] = reinterpret_cast<float(*)[NR][DH]>(st_smem);                                  // in the end, all warps' O
-  float4* s_group = reinterpret_cast<float4*>(st_smem + st_body<DH, NT>());     // per group of 16 keys: k's scale, log2 and reciprocal of v's, page id
+  float4* s_group = reinterpret_cast<float4*>(st_smem + st_body<DH, NT>());     // per group of 16 keys: k's scale, log2 and (unbiased) reciprocal of v's, page id
   __shared__ float s_m[kStWarps][NR], s_l[kStWarps][NR];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int h = blockIdx.x, b = blockIdx.y, chunk_id = blockIdx.z;
@@ -123,7 +125,7 @@ __global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_at
   for (int i = threadIdx.x; i < n_groups; i += kStWarps * 32) {
     const int page = kv8_page(a, s.slot, (k0 + 16 * i) >> a.c.pt_log2);
     const float sv = fmaxf(a.c.vs[(size_t)page * a.c.hkv + h], kv8_pow2(-100));
-    s_group[i] = make_float4(a.c.ks[(size_t)page * a.c.hkv + h], __log2f(sv), 1.f / sv, __int_as_float(page));
+    s_group[i] = make_float4(a.c.ks[(size_t)page * a.c.hkv + h], __log2f(sv), kKv8Unbias / sv, __int_as_float(page));
   }
 
   // Q as the B operand: row g of each tile, d of this lane in the order of the K words; a power of two brings a row's
@@ -167,12 +169,12 @@ __global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_at
 #pragma unroll
   for (int n = 0; n < NT; ++n) { m_ref[n][0] = m_ref[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f; }
 
-  // x[n][4]: (key g, rows 2t, 2t+1), (key g + 8, the same rows), scaled, -inf where hidden.  Turns them into P and returns the
-  // B operand.
+  // x[n][4]: (key g, rows 2t, 2t+1), (key g + 8, the same rows), scaled, -inf where hidden.  Turns them into P (with its
+  // bias) and returns the B operand.
   auto weights = [&](float (&x)[NT][4], uint32_t (&pb)[NT][2]) {
     bool up = false;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) up |= fmaxf(x[n][0], x[n][2]) > m_ref[n][0] + 8.f || fmaxf(x[n][1], x[n][3]) > m_ref[n][1] + 8.f;
+    for (int n = 0; n < NT; ++n) up |= fmaxf(x[n][0], x[n][2]) > m_ref[n][0] + kKv8Rise || fmaxf(x[n][1], x[n][3]) > m_ref[n][1] + kKv8Rise;
     if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -182,7 +184,7 @@ __global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_at
           float mm = fmaxf(x[n][e], x[n][2 + e]);
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
-          const float mn = mm > m_ref[n][e] + 8.f ? mm : m_ref[n][e];
+          const float mn = mm > m_ref[n][e] + kKv8Rise ? mm : m_ref[n][e];
           al[e] = mn == m_ref[n][e] ? 1.f : exp2f(m_ref[n][e] - mn);       // 0 the first time
           m_ref[n][e] = mn;
           l[n][e] *= al[e];
@@ -193,7 +195,7 @@ __global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_at
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float m0 = m_ref[n][0] == -INFINITY ? 0.f : m_ref[n][0], m1 = m_ref[n][1] == -INFINITY ? 0.f : m_ref[n][1];
+      const float m0 = m_ref[n][0] == -INFINITY ? 0.f : m_ref[n][0] - kKv8Bias, m1 = m_ref[n][1] == -INFINITY ? 0.f : m_ref[n][1] - kKv8Bias;
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[n][e] = kv8_ex2(x[n][e] - (e & 1 ? m1 : m0));
       const __half2 p0 = __floats2half2_rn(x[n][0], x[n][1]), p1 = __floats2half2_rn(x[n][2], x[n][3]);
@@ -371,7 +373,7 @@ __global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_at
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) l[n][e & 1] = fmaf(x[n][e], kv8_pow2(-evk[e >> 1]), l[n][e & 1]);
+      for (int e = 0; e < 4; ++e) l[n][e & 1] = fmaf(x[n][e] * kKv8Unbias, kv8_pow2(-evk[e >> 1]), l[n][e & 1]);
 #pragma unroll
     for (int m = 0; m < MT; ++m) {               // d = g * DH/8 + 2m (A rows g) and + 2m + 1 (rows g + 8)
       const uint32_t w0 = vf[0][m], w1 = vf[1][m], w2 = vf[2][m], w3 = vf[3][m];
@@ -403,7 +405,7 @@ __global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_at
 
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();                                // the rings are done with: O takes their place
-  // ---- the warps' parts, joined in warp order
+  // ---- the warps' parts (O without its bias from here on), joined in warp order
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -418,7 +420,7 @@ __global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_at
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        *reinterpret_cast<float2*>(&s_o[warp][2 * t + e + 8 * n][g * (DH / 8) + 2 * m]) = make_float2(o[m][n][e], o[m][n][2 + e]);
+        *reinterpret_cast<float2*>(&s_o[warp][2 * t + e + 8 * n][g * (DH / 8) + 2 * m]) = make_float2(o[m][n][e] * kKv8Unbias, o[m][n][2 + e] * kKv8Unbias);
   __syncthreads();
 #pragma unroll 1
   for (int x = threadIdx.x; x < N * (DH / 4); x += kStWarps * 32) {

@@ -201,6 +201,8 @@ __device__ __forceinline__ void bulk_prefetch(const void* src, uint32_t bytes) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
 
+constexpr float kKuFits = 65504.f;       // the largest fp16: weights whose sum is at most this fit
+
 // Whether all rows of the warp that exist see new row y (causal).
 __device__ __forceinline__ bool ku_all_see(int r, bool on, int rows, int y) { return y < rows && __all_sync(0xffffffffu, !on || y <= r); }
 
@@ -518,9 +520,9 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       const bool cached = j < n_cached;
       const int left = s.len - ((j0 + j) << 7);                              // cached keys from this step on
       // a new reference maximum rescales what O holds, once the half step before has been added to it
-      auto raise = [&](float mt) -> bool {
+      auto raise = [&](float mt, float rise) -> bool {
         float alpha = 1.f;
-        if (mt > m_ref + 8.f) {             // also the first visible key (m_ref = -inf)
+        if (mt > m_ref + rise) {             // also the first visible key (m_ref = -inf)
           alpha = m_ref == -INFINITY ? 1.f : kv8_ex2(m_ref - mt);
           m_ref = mt;
           l *= alpha;
@@ -543,8 +545,8 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       };
       // New rows in one pass against the reference so far, a scale per key; false: a weight was too large, nothing is written.
       auto new_rows_pass = [&]() -> bool {
-        const float mu = m_ref == -INFINITY ? 0.f : m_ref;
-        float sum0 = 0.f, sum1 = 0.f, w0 = 0.f, w1 = 0.f;
+        const float mu = m_ref == -INFINITY ? 0.f : m_ref - kKv8Bias;
+        float w0 = 0.f, w1 = 0.f;
         uint32_t pk[32];
 #pragma unroll
         for (int c0 = 0; c0 < 64; c0 += 16) {
@@ -556,24 +558,26 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
             const float4 c = *reinterpret_cast<const float4*>(scp + c0 + q);      // two keys
             const float p0 = kv8_ex2(fmaf(__uint_as_float(rr[q]), crow * c.x, c.y - mu));
             const float p1 = kv8_ex2(fmaf(__uint_as_float(rr[q + 1]), crow * c.z, c.w - mu));
-            sum0 += p0;
-            sum1 += p1;
             w0 = fmaf(p0, kv8_ex2(-c.y), w0);
             w1 = fmaf(p1, kv8_ex2(-c.w), w1);
             const __half2 v2 = __floats2half2_rn(p0, p1);
             pk[(c0 + q) / 2] = *reinterpret_cast<const uint32_t*>(&v2);
           }
         }
-        const bool fine = !on || (sum0 + sum1 <= 16384.f && m_ref != -INFINITY);
+        uint32_t top = 0;                 // of the weights as fp16 bits: 0x7c00 if one was too large
+#pragma unroll
+        for (int q = 0; q < 32; q += 2) top = __vimax3_u16x2(top, pk[q], pk[q + 1]);
+        const bool fine = !on || (max(top & 0xffffu, top >> 16) < 0x7c00u && m_ref != -INFINITY);
         if (__any_sync(0xffffffffu, !fine)) return false;
-        l += w0 + w1;
+        l += (w0 + w1) * kKv8Unbias;
         tmem_st32(tS + hf * 64, pk);
         return true;
       };
       if (cached && left >= 128) {
-        // 64 cached keys, one set of scales per 16, against the reference so far.  No maximum first: P in fp16 holds up to
-        // 2^16, so only when the half step's weights add up to more than 2^14 (and at the very first) the maximum is taken and the
-        // half step done again.
+        // 64 cached keys, one set of scales per 16, against the reference so far.  No maximum first: only when a weight does not
+        // fit fp16 any more (known from sums of 16, whose limit is a weight 2^7 above the reference or a mean 2^3 above it; and at
+        // the very first) the maximum is taken and the half step done again.  The reference then moves whenever the maximum is
+        // above it, so that the same weights do not come back to this.
         bool first = x == 0;
 #pragma unroll 1
         for (;;) {
@@ -590,13 +594,12 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
               for (int q = 1; q < 15; q += 2) x0 = max3(x0, __uint_as_float(rr[q]), __uint_as_float(rr[q + 1]));
               mt = fmaxf(mt, fmaf(fmaxf(x0, __uint_as_float(rr[15])), crow * c.x, c.y));
             }
-            ok = raise(mt);
+            ok = raise(mt, 0.5f);
             if (!ok) break;
           }
-          const float mu = m_ref == -INFINITY ? 0.f : m_ref;
-          float l_new = l;
+          const float mu = m_ref == -INFINITY ? 0.f : m_ref - kKv8Bias;
+          float l_new = l, top = 0.f;         // top: the largest sum of 16 weights
           uint32_t pk[32];
-          float sum = 0.f;
           {
             // in phases, not element by element: the compiler keeps the order, and 64 exponentials in a row take a warp 600
             // cycles where the interleaved form took 1000 (the special-function unit's own time is 512)
@@ -623,8 +626,8 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
               }
               float l0, l1;
               unpack2(add2(ls, lt), l0, l1);
-              sum += l0 + l1;
-              l_new = fmaf(l0 + l1, kv8_ex2(-scp[g * 16].y), l_new);      // back to the weights alone
+              top = fmaxf(top, l0 + l1);
+              l_new = fmaf((l0 + l1) * kKv8Unbias, kv8_ex2(-scp[g * 16].y), l_new);      // back to the weights alone
             }
 #pragma unroll
             for (int q = 0; q < 32; ++q) {
@@ -632,8 +635,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
               pk[q] = *reinterpret_cast<const uint32_t*>(&v2);
             }
           }
-          const bool fine = sum <= 16384.f;
-          if (first || !__any_sync(0xffffffffu, !fine)) {
+          if (first || !__any_sync(0xffffffffu, top > kKuFits)) {
             l = l_new;
             tmem_st32(tS + hf * 64, pk);    // over the scores it came from
             break;
@@ -656,9 +658,9 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
 #pragma unroll 1
         for (int pass = 0; pass < 2; ++pass) {         // the maximum, then the weights
           if (pass == 1) {
-            ok = raise(mt);
+            ok = raise(mt, kKv8Rise);
             if (!ok) break;
-            mu = m_ref == -INFINITY ? 0.f : m_ref;
+            mu = m_ref == -INFINITY ? 0.f : m_ref - kKv8Bias;
           }
 #pragma unroll 1
           for (int c0 = 0; c0 < 64; c0 += 16) {
@@ -684,7 +686,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
                 }
               }
               if (pass == 1) {
-                l += l0 + l1;
+                l += (l0 + l1) * kKv8Unbias;
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
                   const __half2 v2 = __floats2half2_rn(__uint_as_float(rr[2 * q]), __uint_as_float(rr[2 * q + 1]));
@@ -739,8 +741,8 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
         float o[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          o[q] = f0 == 0.f ? 0.f : __uint_as_float(r0[q]) * f0;
-          if (two && f1 != 0.f) o[q] += __uint_as_float(r1[q]) * f1;
+          o[q] = f0 == 0.f ? 0.f : __uint_as_float(r0[q]) * kKv8Unbias * f0;
+          if (two && f1 != 0.f) o[q] += __uint_as_float(r1[q]) * kKv8Unbias * f1;
         }
         if (bad) {                        // values that are not finite reach exactly the rows that see them
 #pragma unroll 1
