@@ -458,7 +458,8 @@ size_t dart_kv8_attention_workspace_bytes(const dart_kv8_cache* cache, int32_t b
  * Append: row j < n_append[b] of batch entry b -- source row row_index[b][j] of k_new / v_new, or row j -- goes to position
  * seq_lens + j of its slot, for layers first_layer .. first_layer + n_layers - 1 at once.  After a verification the
  * source rows are the accepted path: row_index = its row of dart_verify_out.retrieve.  The pages must be the sequence's
- * own (dart_kv8_reserve); the caller advances seq_lens afterwards.
+ * own (dart_kv8_reserve): this call has no counts to see whether they are, and after a reserve that did not fit they may not
+ * be (dart_kv8_append_owned checks).  The caller advances seq_lens afterwards.
  * Scale of a page and head: the smallest power of two s >= 2^-64 with |x| <= qmax * s (qmax 448 or 127) over the finite
  * new values that the call writes there, or the page's scale if the sequence already has rows in it and that is larger;
  * codes are x / s rounded to nearest even (exact division, one rounding).  A scale that grows re-rounds the page's
@@ -487,7 +488,7 @@ int dart_kv8_append(const dart_kv8_cache* cache, const dart_kv8_append_in* in, v
 /*
  * Bookkeeping of a pool: which pages each sequence slot holds, and how many table entries name each page (0: free).
  * All three arrays are the caller's; a pool starts with table -1, lengths 0, counts 0.  Sequences share pages after a
- * fork; a shared page is never written (reserve replaces it first).  Lists name slots; a slot or pair that is out of
+ * fork; a shared page is not to be written (reserve replaces it first; dart_kv8_append_owned leaves it alone).  Lists name slots; a slot or pair that is out of
  * range, named twice, or (fork) has a source that is also a destination or a destination in use, is skipped and reported.
  */
 typedef struct dart_kv8_pages {
@@ -498,6 +499,13 @@ typedef struct dart_kv8_pages {
   int32_t* seq_lens;         /* DEVICE i32 [max_seqs] */
   int32_t* ref_count;        /* DEVICE i32 [n_pages] */
 } dart_kv8_pages;
+/*
+ * dart_kv8_append that looks at the counts: rows go only into pages that no other slot names (count 1); the others are left
+ * as they are and reported (DART_ERR_INVALID_ARG, unless the status word already holds an error).  For callers that do not
+ * wait for the status of the dart_kv8_reserve before it: when that did not fit, the table still names the shared page.
+ * in->page_table, max_seqs and max_pages are those of `pages`.
+ */
+int dart_kv8_append_owned(const dart_kv8_cache* cache, const dart_kv8_pages* pages, const dart_kv8_append_in* in, void* cuda_stream);
 /* Slot dst[i] becomes a copy of slot src[i] (length, and the pages that hold its tokens, shared).  n: 1..1024 pairs. */
 int dart_kv8_fork(const dart_kv8_pages* pages, const int32_t* src, const int32_t* dst, int32_t n, int32_t* status, void* cuda_stream);
 /*

@@ -30,7 +30,7 @@ EXPORTS = [
     "dart_draft_init", "dart_draft_step", "dart_build_tree", "dart_draft_destroy", "dart_last_device_status",
     "dart_last_cuda_error", "dart_status_string", "dart_workspace_bytes", "dart_ngram_bytes", "dart_train_attention_fwd", "dart_step_launch_count", "dart_draft_prefill", "dart_tree_verify_inputs",
     "dart_set_profile_events", "dart_topk_rows_noalloc", "dart_selftest_bounded_wait", "dart_draft_step_host",
-    "dart_kv8_attention", "dart_kv8_attention_workspace_bytes", "dart_kv8_append", "dart_kv8_fork", "dart_kv8_reserve", "dart_kv8_release",
+    "dart_kv8_attention", "dart_kv8_attention_workspace_bytes", "dart_kv8_append", "dart_kv8_append_owned", "dart_kv8_fork", "dart_kv8_reserve", "dart_kv8_release",
     "dart_kv8_compact", "dart_kv8_pages_workspace_bytes",
 ]
 
@@ -189,12 +189,13 @@ def lib() -> C.CDLL:
         L.dart_kv8_attention.argtypes = [P, P, P]
         L.dart_kv8_attention_workspace_bytes.argtypes = [P, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         L.dart_kv8_append.argtypes = [P, P, P]
+        L.dart_kv8_append_owned.argtypes = [P, P, P, P]
         L.dart_kv8_fork.argtypes = [P, P, P, C.c_int32, P, P]
         L.dart_kv8_release.argtypes = [P, P, C.c_int32, P, P]
         L.dart_kv8_reserve.argtypes = [P, P, P, P, C.c_int32, P, C.c_size_t, P, P]
         L.dart_kv8_compact.argtypes = [P, P, P, P, C.c_size_t, P, P]
         L.dart_kv8_pages_workspace_bytes.argtypes = [P]
-        for name in ("attention", "append", "fork", "release", "reserve", "compact"):
+        for name in ("attention", "append", "append_owned", "fork", "release", "reserve", "compact"):
             getattr(L, "dart_kv8_" + name).restype = C.c_int
         L.dart_kv8_attention_workspace_bytes.restype = L.dart_kv8_pages_workspace_bytes.restype = C.c_size_t
         _lib = L
@@ -506,9 +507,10 @@ def kv8_attention(cache: Kv8Cache, layer: int, q: torch.Tensor, k_new: Optional[
 def kv8_append(cache: Kv8Cache, first_layer: int, k_new: torch.Tensor, v_new: torch.Tensor, seq_lens: torch.Tensor,
                page_table: torch.Tensor, *, n_append: Optional[torch.Tensor] = None, row_index: Optional[torch.Tensor] = None,
                max_append: Optional[int] = None, slots: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
-               stream=None) -> None:
+               pages: Optional[Kv8Pages] = None, stream=None) -> None:
     """dart_kv8_append: k_new, v_new bf16 [n_layers, batch, rows, n_kv_heads, head_dim]; row_index int32 [batch, max_append] (an
-    accepted path of dart_tree_verify_inputs) or None: the rows in order.  The caller advances seq_lens."""
+    accepted path of dart_tree_verify_inputs) or None: the rows in order.  The caller advances seq_lens.  With `pages` (whose
+    page_table is then meant) dart_kv8_append_owned: pages that other sequences share are left alone and reported."""
     dev = cache.index
     if k_new.dim() != 5 or v_new.shape != k_new.shape:
         raise ValueError("k_new and v_new: [n_layers, batch, rows, n_kv_heads, head_dim] are needed, of one shape")
@@ -535,7 +537,10 @@ def kv8_append(cache: Kv8Cache, first_layer: int, k_new: torch.Tensor, v_new: to
                          _kv8_check(seq_lens, "seq_lens", _I32, dev, (S,)), _kv8_check(page_table, "page_table", _I32, dev),
                          _kv8_check(n_append, "n_append", _I32, dev, (B,)), _kv8_check(row_index, "row_index", _I32, dev, (B, A)),
                          _kv8_check(status, "status", _I32, dev))
-    _kv8_call("dart_kv8_append", dev, stream, cache.ref, a)
+    if pages is None:
+        return _kv8_call("dart_kv8_append", dev, stream, cache.ref, a)
+    _kv8_same_pool(pages, cache)
+    _kv8_call("dart_kv8_append_owned", dev, stream, cache.ref, pages.ref, a)
 
 
 def kv8_pages_workspace_bytes(pages: Kv8Pages) -> int:

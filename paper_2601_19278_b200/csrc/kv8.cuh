@@ -37,6 +37,7 @@ struct Kv8AppendArgs {
   long long row_stride, layer_stride;
   const bf16 *k_new, *v_new;
   const int *slots, *seq_lens, *table, *n_append, *row_index;
+  const int* ref;                          // null: every page in the table is the sequence's own
   int* status;
 };
 
@@ -87,6 +88,11 @@ size_t kv8_pages_workspace(int n_pages);
 
 __device__ __forceinline__ void kv8_report(int* status, int code) {
   if (status != nullptr) atomicExch(status, code);
+}
+
+// The same where an earlier error says more: a page that is missing because a reserve did not fit.
+__device__ __forceinline__ void kv8_report_first(int* status, int code) {
+  if (status != nullptr) atomicCAS(status, 0, code);
 }
 
 // What batch entry b works on.  A bad slot, length or row count reads as an empty sequence and is reported by `report`.

@@ -110,7 +110,7 @@ int dart_kv8_attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, 
   return e == cudaSuccess ? DART_OK : fail(e);
 }
 
-int dart_kv8_append(const dart_kv8_cache* cache, const dart_kv8_append_in* in, void* cuda_stream) {
+static int append(const dart_kv8_cache* cache, const dart_kv8_append_in* in, const int32_t* ref, void* cuda_stream) {
   if (in == nullptr || !cache_ok(cache)) return DART_ERR_INVALID_ARG;
   const int pt = cache->page_tokens, dh = cache->head_dim;
   if (in->first_layer < 0 || in->n_layers < 1 || in->first_layer > cache->n_layers - in->n_layers || in->batch < 1 || in->batch > 1024 ||
@@ -139,9 +139,21 @@ int dart_kv8_append(const dart_kv8_cache* cache, const dart_kv8_append_in* in, v
   a.row_stride = in->row_stride; a.layer_stride = in->layer_stride;
   a.k_new = static_cast<const bf16*>(in->k_new); a.v_new = static_cast<const bf16*>(in->v_new);
   a.slots = in->slots; a.seq_lens = in->seq_lens; a.table = in->page_table; a.n_append = in->n_append; a.row_index = in->row_index;
+  a.ref = ref;
   a.status = in->status;
   const cudaError_t e = launch_kv8_append(a, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? DART_OK : fail(e);
+}
+
+int dart_kv8_append(const dart_kv8_cache* cache, const dart_kv8_append_in* in, void* cuda_stream) {
+  return append(cache, in, nullptr, cuda_stream);
+}
+
+int dart_kv8_append_owned(const dart_kv8_cache* cache, const dart_kv8_pages* pages, const dart_kv8_append_in* in, void* cuda_stream) {
+  if (!pages_ok(pages) || !cache_ok(cache) || in == nullptr || cache->n_pages != pages->n_pages || cache->page_tokens != pages->page_tokens ||
+      in->max_seqs != pages->max_seqs || in->max_pages != pages->max_pages || in->page_table != pages->page_table)
+    return DART_ERR_INVALID_ARG;
+  return append(cache, in, pages->ref_count, cuda_stream);
 }
 
 size_t dart_kv8_pages_workspace_bytes(const dart_kv8_pages* pages) {

@@ -108,14 +108,19 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
   };
   auto store = [&](int col, const Unit& x) {
     if (x.page < 0 || x.page >= a.n_pages) {
-      if (tid == 0) kv8_report(a.status, KV8_BAD_ARG);
+      if (tid == 0) kv8_report_first(a.status, KV8_BAD_ARG);
       return;
     }
     const size_t ph = ((size_t)layer * a.n_pages + x.page) * a.hkv + h;
     uint8_t* codes = (is_v ? a.v : a.k) + ph * a.pt * DH;
     float* scale = (is_v ? a.vs : a.ks) + ph;
     const bool held = col * a.pt < len;            // the page already holds rows of the sequence
+    const int names = a.ref != nullptr ? a.ref[x.page] : 1;
     const float was = held ? *scale : 0.f;
+    if (names != 1) {                              // other sequences read this page (or nobody holds it)
+      if (tid == 0) kv8_report_first(a.status, KV8_BAD_ARG);
+      return;
+    }
     // the largest |x|: bits of both halves of all words, a three-way 16-bit maximum per two words
     uint32_t top = 0;
 #pragma unroll
