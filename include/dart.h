@@ -453,6 +453,13 @@ typedef struct dart_kv8_attn_in {
 int dart_kv8_attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, void* cuda_stream);
 /* Workspace for this shape and any smaller max_len; 0 for arguments dart_kv8_attention refuses. */
 size_t dart_kv8_attention_workspace_bytes(const dart_kv8_cache* cache, int32_t batch, int32_t rows, int32_t n_q_heads, int32_t max_len);
+/*
+ * Self-test of the time-out path, as dart_selftest_bounded_wait: an attention call for many rows (the tcgen05 kernel; others
+ * are refused) in which the keys of every CTA stop arriving at their missing_from-th group of 64, and every wait gives up after
+ * spin_limit tries (1 .. 100000, of up to about 1.3 microseconds each).  in->status becomes DART_ERR_TIMEOUT, `out` is void, the
+ * next call is unharmed.  Faults nothing, hangs nothing.
+ */
+int dart_selftest_kv8_wait(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, int32_t spin_limit, int32_t missing_from, void* cuda_stream);
 
 /*
  * Append: row j < n_append[b] of batch entry b -- source row row_index[b][j] of k_new / v_new, or row j -- goes to position

@@ -62,7 +62,10 @@ struct Kv8Plan {
   int paired;            // tiles 2p and 2p + 1 go together, an odd last one alone; else every tile alone
   float *o_part, *ml_part;
   size_t bytes;          // of workspace
+  int spin;              // umma: tries of a bounded wait, of up to about 1.3 us each
+  int withhold;          // umma: K's copies stop at this 64-key slot of every CTA (the self-test of the waits); -1: they do not
 };
+constexpr int kKv8Spin = 1000000;
 
 // A long axis in equal parts: n CTAs of `per` (keys or steps) each, the last one shorter.
 struct Kv8Split { int n, per; };
@@ -76,7 +79,8 @@ __host__ __device__ inline Kv8Split kv8_split_keys(int len, int chunk) { return 
 
 cudaError_t launch_kv8_attn_umma(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStream_t st);
 void kv8_umma_plan(const Kv8AttnArgs& a, Kv8Plan& p);
-cudaError_t launch_kv8_attention(const Kv8AttnArgs& a, void* workspace, cudaStream_t st);
+cudaError_t launch_kv8_attention(const Kv8AttnArgs& a, void* workspace, int spin, int withhold, cudaStream_t st);
+bool kv8_attention_many_rows(const Kv8AttnArgs& a);
 size_t kv8_attention_workspace(const Kv8AttnArgs& a);
 cudaError_t launch_kv8_append(const Kv8AppendArgs& a, cudaStream_t st);
 cudaError_t launch_kv8_fork(const Kv8PagesArgs& p, const int* src, const int* dst, int n, int* status, cudaStream_t st);

@@ -78,7 +78,7 @@ size_t dart_kv8_attention_workspace_bytes(const dart_kv8_cache* cache, int32_t b
   return kv8_attention_workspace(attn_shape(cache, batch, rows, n_q_heads, max_len));
 }
 
-int dart_kv8_attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, void* cuda_stream) {
+static int attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, bool selftest, int spin, int withhold, void* cuda_stream) {
   if (in == nullptr || !cache_ok(cache) || !attn_shape_ok(cache, in->batch, in->rows, in->n_q_heads, in->max_len)) return DART_ERR_INVALID_ARG;
   const int pt = cache->page_tokens, dh = cache->head_dim;
   if (in->layer < 0 || in->layer >= cache->n_layers || !table_ok(in->max_seqs, in->max_pages, pt)) return DART_ERR_INVALID_ARG;
@@ -94,6 +94,7 @@ int dart_kv8_attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, 
     return DART_ERR_INVALID_ARG;
   Kv8AttnArgs a = attn_shape(cache, in->batch, in->rows, in->n_q_heads, in->max_len);
   if (!aligned16(in->workspace) || in->workspace_bytes < kv8_attention_workspace(a)) return DART_ERR_INVALID_ARG;
+  if (selftest && !kv8_attention_many_rows(a)) return DART_ERR_INVALID_ARG;
   const int arch = check_arch();
   if (arch != DART_OK) return arch;
   const size_t layer = (size_t)in->layer * cache->n_pages * cache->n_kv_heads;
@@ -106,8 +107,17 @@ int dart_kv8_attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, 
   a.q = static_cast<const bf16*>(in->q); a.k_new = static_cast<const bf16*>(in->k_new); a.v_new = static_cast<const bf16*>(in->v_new);
   a.slots = in->slots; a.seq_lens = in->seq_lens; a.table = in->page_table; a.n_rows = in->n_rows; a.mask = in->mask;
   a.out = static_cast<bf16*>(in->out); a.status = in->status;
-  const cudaError_t e = launch_kv8_attention(a, in->workspace, static_cast<cudaStream_t>(cuda_stream));
+  const cudaError_t e = launch_kv8_attention(a, in->workspace, spin, withhold, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? DART_OK : fail(e);
+}
+
+int dart_kv8_attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, void* cuda_stream) {
+  return attention(cache, in, false, kKv8Spin, -1, cuda_stream);
+}
+
+int dart_selftest_kv8_wait(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, int32_t spin_limit, int32_t missing_from, void* cuda_stream) {
+  if (in == nullptr || in->status == nullptr || spin_limit < 1 || spin_limit > 100000 || missing_from < 0) return DART_ERR_INVALID_ARG;
+  return attention(cache, in, true, spin_limit, missing_from, cuda_stream);
 }
 
 static int append(const dart_kv8_cache* cache, const dart_kv8_append_in* in, const int32_t* ref, void* cuda_stream) {

@@ -590,10 +590,13 @@ cudaError_t launch_stream_rows(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStrea
 
 }  // namespace
 
+bool kv8_attention_many_rows(const Kv8AttnArgs& a) { return make_plan(a, nullptr).umma != 0; }
 size_t kv8_attention_workspace(const Kv8AttnArgs& a) { return make_plan(a, nullptr).bytes; }
 
-cudaError_t launch_kv8_attention(const Kv8AttnArgs& a, void* workspace, cudaStream_t st) {
-  const Kv8Plan p = make_plan(a, workspace);
+cudaError_t launch_kv8_attention(const Kv8AttnArgs& a, void* workspace, int spin, int withhold, cudaStream_t st) {
+  Kv8Plan p = make_plan(a, workspace);
+  p.spin = spin;
+  p.withhold = withhold;
   cudaError_t e;
   if (p.umma)
     e = launch_kv8_attn_umma(a, p, st);

@@ -41,28 +41,32 @@ constexpr int kKuBad = 4096 / 32;
 // Bounded wait in little code (the loop is not unrolled: there are some twenty of them).  try_wait suspends the warp for up to
 // 2600 cycles (measured), which leaves the issue slots to the softmax warps beside it (1 % of the kernel's time against
 // test_wait, with or without a pause between two looks; with a suspend-time hint, or a look at the clock, 2 to 3 % slower).
-// A million tries, about a second and a half, then the CTA's abort flag is raised and all roles leave.
-__device__ __forceinline__ bool ku_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+// `patience`, in shared memory, is how many tries every wait of the CTA has (plan.spin); the wait that runs out sets it to 0 and
+// all roles leave.  (As an argument of the kernel the limit took a register that the softmax warps do not have: 16 trees 178 us,
+// the prompt chunk 287, here 174.5 and 267.)  A whole warp waits and one answer is every lane's, since what follows has
+// instructions that all lanes have to meet; the votes take no time that shows.
+__device__ __forceinline__ bool ku_wait(uint64_t* bar, uint32_t parity, volatile int* patience) {
 #pragma unroll 1
-  for (int it = 0; it < 1000000; ++it) {
+  for (int it = 0;; ++it) {
     uint32_t ok;
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                  : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
-    if (ok) return true;
-    if (*abort_flag) return false;
+    if (__all_sync(0xffffffffu, ok)) return true;
+    if (__any_sync(0xffffffffu, it >= *patience)) break;
   }
-  *abort_flag = 1;
+  *patience = 0;
   return false;
 }
 
 // What is not an operand tile or a code slot.
 struct KuShared {
   uint64_t q_full[2], c_full[2][kKuSingleSlots], c_empty[2][kKuSingleSlots], k_full[2], k_empty[2], v_full[2], v_empty[2], sc_full[2];
-  uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];
+  uint64_t s_full[2][2], p_full[2][2], pv_done[2][2], drained[2];
   float2 sc[2][128];                     // per key of a step: scale of k, log2 of v's
   uint32_t bad[kKuBad];                  // new rows with a v value that is not finite
   uint32_t tmem_base;
-  int abort_flag, any_bad;
+  int patience, any_bad;
+  int2 issued[2];                        // code slots that the producers of K and V asked for; slots of a ring
 };
 // Two row tiles: Q, Q, K, K, V, V and two slots a ring; one: Q, K, K, V, V, three slots a ring and the pipelines' (m, l).  With
 // DH = 128 the first form is all that a block can have.
@@ -218,7 +222,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
   auto &s_full = sh.s_full, &p_full = sh.p_full, &pv_done = sh.pv_done;
   auto& s_sc = sh.sc;
   auto& s_bad = sh.bad;
-  int& abort_flag = sh.abort_flag;
+  int& patience = sh.patience;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = blockIdx.x, b = blockIdx.y;
   const Kv8Seq s = kv8_seq(a, b, tid == 0 && h == 0 && blockIdx.z == 0);
@@ -255,9 +259,10 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       mbar_init(&k_full[i], 4); mbar_init(&k_empty[i], pair ? 2 : 1);      // one release per pipeline that reads the buffer
       mbar_init(&v_full[i], 4); mbar_init(&v_empty[i], pair ? 2 : 1);
       mbar_init(&sc_full[i], 4);
+      mbar_init(&sh.drained[i], 1);
       for (int hf = 0; hf < 2; ++hf) { mbar_init(&s_full[i][hf], 1); mbar_init(&p_full[i][hf], 4); mbar_init(&pv_done[i][hf], 1); }
     }
-    abort_flag = 0;
+    patience = plan.spin;
     sh.any_bad = 0;
     fence_barrier_init();
   }
@@ -280,7 +285,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
     // has a warp of its own, and page ids are read 32 at a time, the next 32 on their way.
     const int is_v = __shfl_sync(0xffffffffu, warp >> 1, 0);
     const int pages = a.c.pt_log2 < 6 ? 64 >> a.c.pt_log2 : 1, bytes = (64 / pages) * DH;      // copies per slot, bytes each
-    const int total = 2 * n_cached, col0 = (int)(((long long)j0 << 7) >> a.c.pt_log2), n_cols = (s.len + a.c.pt - 1) >> a.c.pt_log2;
+    const int total = is_v || plan.withhold < 0 ? 2 * n_cached : min(2 * n_cached, plan.withhold), col0 = (int)(((long long)j0 << 7) >> a.c.pt_log2), n_cols = (s.len + a.c.pt - 1) >> a.c.pt_log2;
     const size_t page_bytes = (size_t)a.c.hkv * a.c.pt * DH;
     const uint8_t* base = (is_v ? a.c.v : a.c.k) + (size_t)h * a.c.pt * DH;
     uint8_t* ring = sC + is_v * n_slots * Ly::slot;
@@ -300,7 +305,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
         ids_next = ids_at(window + 1);
       }
       const int page = __shfl_sync(0xffffffffu, ids, (col + lane) & 31);
-      if (use > 0 && !ku_wait(&empty[st], (use - 1) & 1, &abort_flag)) break;
+      if (use > 0 && !ku_wait(&empty[st], (use - 1) & 1, &patience)) break;
       if (lane == 0) mbar_expect_tx(&full[st], max(live, 0) * bytes);      // 0: the slot lies behind the end, the phase completes
       __syncwarp();
       // two slots are little time for the way from HBM: the lines two steps on are asked into L2
@@ -310,11 +315,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       if (lane < live) bulk_load(ring + st * Ly::slot + lane * bytes, base + page * page_bytes + (key & (a.c.pt - 1)) * DH, bytes, &full[st]);
       if (++st == n_slots) { st = 0; ++use; }
     }
-    if (abort_flag)                  // leave no copy in flight behind
-#pragma unroll 1
-      for (int u = max(0, t - n_slots); u < t; ++u)
-#pragma unroll 1
-        for (int it = 0; it < 1000000 && !mbar_test_wait(&full[u % n_slots], (u / n_slots) & 1); ++it) {}
+    if (lane == 0) sh.issued[is_v] = make_int2(t, n_slots);
    } else {
     // ---- MMA issuer of pipeline p.  The whole warp runs the loop and one elected lane issues, so descriptors and control
     // flow stay in uniform registers.
@@ -324,7 +325,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
     const uint64_t dq = desc_sw128(smem_u32(sQ + (pair ? p : 0) * Ly::tile));
     const uint64_t dk = desc_sw128(smem_u32(sK)), dv = desc_sw128_mn(smem_u32(sV), 16384);
     const uint32_t tS = tmem + p * 256, tO = tS + 128;
-    bool ok = nh == 0 || ku_wait(&q_full[pair ? p : 0], 0, &abort_flag);
+    bool ok = nh == 0 || ku_wait(&q_full[pair ? p : 0], 0, &patience);
     // Two things to issue, in whichever order they come ready: S of half step y, once its K is there and P of half y - 2,
     // which lies where it goes, has been used; O += P V of half x, once P is there.  (Waiting for one before the other
     // cost a thousand cycles a half step.)
@@ -369,8 +370,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
         }
       }
       if (it > 0) {
-        if (__any_sync(0xffffffffu, *(volatile int*)&abort_flag != 0)) break;
-        if (it > 4000000) { abort_flag = 1; break; }
+        if (__any_sync(0xffffffffu, it > 4 * *(volatile int*)&patience)) { patience = 0; break; }
         __nanosleep(20);
       }
     }
@@ -409,7 +409,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
 #pragma unroll 1
     for (int j = 0; j < n && ok; ++j) {
       const int buf = j & 1, use = j >> 1;
-      if (use > 0) ok = ku_wait(&empty[buf], (use - 1) & 1, &abort_flag);
+      if (use > 0) ok = ku_wait(&empty[buf], (use - 1) & 1, &patience);
       if (!ok) break;
       if (j < n_cached) {
         if (is_v) {
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
 #pragma unroll 1
         for (int q = 0; q < 2; ++q) {        // 64 keys each
           uint8_t* tile = tiles + buf * Ly::tile + q * 8192;
-          ok = ku_wait(&c_full[is_v][st], round & 1, &abort_flag);
+          ok = ku_wait(&c_full[is_v][st], round & 1, &patience);
           if (!ok) break;
           const uint8_t* src = ring + st * Ly::slot + from;
           uint2 w[4][DH / 64];
@@ -513,7 +513,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
     bool ok = true;
     for (int x = 0; x < 2 * np; ++x) {        // half steps of 64 keys
       const int i = x >> 1, hf = x & 1, j = step_of(p, i), buf = j & 1;
-      ok = (hf == 1 || ku_wait(&sc_full[buf], (j >> 1) & 1, &abort_flag)) && ku_wait(&s_full[p][hf], i & 1, &abort_flag);
+      ok = (hf == 1 || ku_wait(&sc_full[buf], (j >> 1) & 1, &patience)) && ku_wait(&s_full[p][hf], i & 1, &patience);
       if (!ok) break;
       tc_fence_after();
       const float2* scp = &s_sc[buf][hf * 64];
@@ -528,7 +528,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
           l *= alpha;
         }
         if (x > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
-          if (!ku_wait(&pv_done[p][hf ^ 1], (hf ? i : i - 1) & 1, &abort_flag)) return false;
+          if (!ku_wait(&pv_done[p][hf ^ 1], (hf ? i : i - 1) & 1, &patience)) return false;
           tc_fence_after();
 #pragma unroll 1
           for (int cb = 0; cb < DH; cb += 16) {
@@ -704,7 +704,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       __syncwarp();
       if (lane == 0) mbar_arrive(&p_full[p][hf]);
     }
-    if (ok && np > 0) ok = ku_wait(&pv_done[p][1], (np - 1) & 1, &abort_flag);
+    if (ok && np > 0) ok = ku_wait(&pv_done[p][1], (np - 1) & 1, &patience);
     if (!pair) {
       s_ml[p][row] = make_float2(m_ref, l);
       tc_fence_before();
@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
     }
     tc_fence_after();
     // ---- results: a pipeline's own tile, or the join of the two pipelines of a single tile (half of the columns each)
-    if (!abort_flag) {
+    if (__all_sync(0xffffffffu, *(volatile int*)&patience)) {
       const uint32_t tR = tmem + ((uint32_t)(wq * 32) << 16) + 128;
       const bool two = !pair && n > 1;
       const float2 ml0 = pair ? make_float2(m_ref, l) : s_ml[0][row], ml1 = two ? s_ml[1][row] : make_float2(-INFINITY, 0.f);
@@ -779,8 +779,25 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
   }
   tc_fence_before();
   __syncthreads();
+  if (patience == 0) {             // a wait ran out: leave no copy and no MMA in flight behind
+    tc_fence_after();
+    if (warp == 0 || warp == 2) {
+      const int2 last = sh.issued[warp >> 1];
+#pragma unroll 1
+      for (int u = max(0, last.x - last.y); u < last.x; ++u)
+#pragma unroll 1
+        for (int it = 0; it < 1000000 && !mbar_test_wait(&c_full[warp >> 1][u % last.y], (u / last.y) & 1); ++it) {}
+    } else if (warp == 1 || warp == 3) {
+      if (elect_one()) mma_commit(&sh.drained[warp >> 1]);
+      __syncwarp();
+#pragma unroll 1
+      for (int it = 0; it < 1000000 && !mbar_test_wait(&sh.drained[warp >> 1], 0); ++it) {}
+    }
+    if (tid == 0) kv8_report(a.status, DEV_TIMEOUT);
+    tc_fence_before();
+    __syncthreads();
+  }
   if (warp == 2) { tc_fence_after(); tmem_dealloc(tmem, 512); }
-  if (abort_flag && tid == 0) kv8_report(a.status, DEV_TIMEOUT);
 }
 
 // Key steps of a CTA.  A CTA's start and end (queries, the first copies, the first scores, its result) cost as much as five or
