@@ -432,7 +432,8 @@ typedef struct dart_kv8_attn_in {
   int32_t n_q_heads;         /* a multiple of n_kv_heads, at most 128 per KV head */
   int32_t max_seqs;          /* rows of page_table and seq_lens; >= batch without slots */
   int32_t max_pages;         /* columns of page_table */
-  int32_t max_len;           /* HOST bound of seq_lens, 0 .. max_pages * page_tokens: sizes the launch and the workspace */
+  int32_t max_len;           /* HOST bound of seq_lens, 0 .. max_pages * page_tokens: sizes the launch and the workspace; keep it
+                                near the longest length (dart_kv8_attention_plan) */
   const void* q;             /* DEVICE bf16 [batch, R, n_q_heads, head_dim], RoPE applied */
   const void* k_new;         /* DEVICE bf16 [batch, R, n_kv_heads, head_dim] or NULL (then v_new and mask are NULL too) */
   const void* v_new;
@@ -452,7 +453,20 @@ typedef struct dart_kv8_attn_in {
 } dart_kv8_attn_in;
 int dart_kv8_attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, void* cuda_stream);
 /* Workspace for this shape and any smaller max_len; 0 for arguments dart_kv8_attention refuses. */
-size_t dart_kv8_attention_workspace_bytes(const dart_kv8_cache* cache, int32_t batch, int32_t rows, int32_t n_q_heads, int32_t max_len);
+size_t dart_kv8_attention_workspace_bytes(const dart_kv8_cache* cache, int32_t batch, int32_t rows, int32_t n_q_heads, int32_t max_len);/*
+ * How such a call is cut into CTAs.  The key axis is split by max_len, not by the lengths on the device: with a bound far above
+ * them the parts are as long as the bound asks for and few of them have work, so a tight max_len is a faster call.
+ */
+typedef struct dart_kv8_plan {
+  int32_t many_rows;         /* 1: the tcgen05 kernel, 0: the streaming kernel for few rows of a KV head */
+  int32_t row_tiles;         /* many rows: tiles of 128 (row, head of the group) pairs */
+  int32_t paired;            /* many rows: two tiles share a CTA (an odd last one has its own, with twice the keys) */
+  int32_t keys_per_part;     /* keys, new rows included where many_rows, that a CTA takes at most */
+  int32_t max_parts;         /* CTAs that share a KV head's keys at length max_len; 1: no join */
+} dart_kv8_plan;
+int dart_kv8_attention_plan(const dart_kv8_cache* cache, int32_t batch, int32_t rows, int32_t n_q_heads, int32_t max_len, int32_t with_new_rows,
+                            dart_kv8_plan* out);
+
 /*
  * Self-test of the time-out path, as dart_selftest_bounded_wait: an attention call for many rows (the tcgen05 kernel; others
  * are refused) in which the keys of every CTA stop arriving at their missing_from-th group of 64, and every wait gives up after

@@ -32,6 +32,7 @@ EXPORTS = [
     "dart_set_profile_events", "dart_topk_rows_noalloc", "dart_selftest_bounded_wait", "dart_draft_step_host",
     "dart_kv8_attention", "dart_kv8_attention_workspace_bytes", "dart_kv8_append", "dart_kv8_append_owned", "dart_kv8_fork", "dart_kv8_reserve", "dart_kv8_release",
     "dart_kv8_compact", "dart_kv8_pages_workspace_bytes", "dart_selftest_kv8_wait",
+    "dart_kv8_attention_plan",
 ]
 
 
@@ -132,6 +133,10 @@ class DartKv8AppendIn(C.Structure):
                 ("n_append", C.c_void_p), ("row_index", C.c_void_p), ("status", C.c_void_p)]
 
 
+class DartKv8Plan(C.Structure):
+    _fields_ = [("many_rows", C.c_int32), ("row_tiles", C.c_int32), ("paired", C.c_int32), ("keys_per_part", C.c_int32), ("max_parts", C.c_int32)]
+
+
 class DartKv8Pages(C.Structure):
     _fields_ = [("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("max_seqs", C.c_int32), ("max_pages", C.c_int32),
                 ("page_table", C.c_void_p), ("seq_lens", C.c_void_p), ("ref_count", C.c_void_p)]
@@ -188,6 +193,8 @@ def lib() -> C.CDLL:
         P = C.c_void_p
         L.dart_kv8_attention.argtypes = [P, P, P]
         L.dart_kv8_attention_workspace_bytes.argtypes = [P, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+        L.dart_kv8_attention_plan.argtypes = [P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, P]
+        L.dart_kv8_attention_plan.restype = C.c_int
         L.dart_kv8_append.argtypes = [P, P, P]
         L.dart_kv8_append_owned.argtypes = [P, P, P, P]
         L.dart_kv8_fork.argtypes = [P, P, P, C.c_int32, P, P]
@@ -471,6 +478,16 @@ class Kv8Pages:
 
 def kv8_attention_workspace_bytes(cache: Kv8Cache, batch: int, rows: int, n_q_heads: int, max_len: int) -> int:
     return lib().dart_kv8_attention_workspace_bytes(cache.ref, batch, rows, n_q_heads, max_len)
+
+
+def kv8_attention_plan(cache: Kv8Cache, batch: int, rows: int, n_q_heads: int, max_len: int, new_rows: bool = True) -> Dict[str, int]:
+    """dart_kv8_attention_plan: which kernel a call of this shape runs on and how its key axis is split (by max_len: a bound near the
+    longest length is a faster call)."""
+    p = DartKv8Plan()
+    rc = lib().dart_kv8_attention_plan(cache.ref, batch, rows, n_q_heads, max_len, int(new_rows), C.byref(p))
+    if rc != DART_OK:
+        raise DartError(rc, "dart_kv8_attention_plan")
+    return {f[0]: getattr(p, f[0]) for f in p._fields_}
 
 
 def kv8_attention(cache: Kv8Cache, layer: int, q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: Optional[torch.Tensor],

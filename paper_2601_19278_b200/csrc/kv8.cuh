@@ -80,7 +80,7 @@ __host__ __device__ inline Kv8Split kv8_split_keys(int len, int chunk) { return 
 cudaError_t launch_kv8_attn_umma(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStream_t st);
 void kv8_umma_plan(const Kv8AttnArgs& a, Kv8Plan& p);
 cudaError_t launch_kv8_attention(const Kv8AttnArgs& a, void* workspace, int spin, int withhold, cudaStream_t st);
-bool kv8_attention_many_rows(const Kv8AttnArgs& a);
+Kv8Plan kv8_attention_plan(const Kv8AttnArgs& a);
 size_t kv8_attention_workspace(const Kv8AttnArgs& a);
 cudaError_t launch_kv8_append(const Kv8AppendArgs& a, cudaStream_t st);
 cudaError_t launch_kv8_fork(const Kv8PagesArgs& p, const int* src, const int* dst, int n, int* status, cudaStream_t st);

@@ -78,6 +78,17 @@ size_t dart_kv8_attention_workspace_bytes(const dart_kv8_cache* cache, int32_t b
   return kv8_attention_workspace(attn_shape(cache, batch, rows, n_q_heads, max_len));
 }
 
+int dart_kv8_attention_plan(const dart_kv8_cache* cache, int32_t batch, int32_t rows, int32_t n_q_heads, int32_t max_len, int32_t with_new_rows,
+                            dart_kv8_plan* out) {
+  if (out == nullptr || !attn_shape_ok(cache, batch, rows, n_q_heads, max_len)) return DART_ERR_INVALID_ARG;
+  Kv8AttnArgs a = attn_shape(cache, batch, rows, n_q_heads, max_len);
+  static const bf16 some_row{};
+  if (with_new_rows) a.k_new = &some_row;      // (never read)
+  const Kv8Plan p = kv8_attention_plan(a);
+  *out = dart_kv8_plan{p.umma, p.umma ? p.n_tiles : 0, p.paired, p.umma ? p.chunk * 128 : p.chunk, p.max_chunks};
+  return DART_OK;
+}
+
 static int attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, bool selftest, int spin, int withhold, void* cuda_stream) {
   if (in == nullptr || !cache_ok(cache) || !attn_shape_ok(cache, in->batch, in->rows, in->n_q_heads, in->max_len)) return DART_ERR_INVALID_ARG;
   const int pt = cache->page_tokens, dh = cache->head_dim;
@@ -94,7 +105,7 @@ static int attention(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, bo
     return DART_ERR_INVALID_ARG;
   Kv8AttnArgs a = attn_shape(cache, in->batch, in->rows, in->n_q_heads, in->max_len);
   if (!aligned16(in->workspace) || in->workspace_bytes < kv8_attention_workspace(a)) return DART_ERR_INVALID_ARG;
-  if (selftest && !kv8_attention_many_rows(a)) return DART_ERR_INVALID_ARG;
+  if (selftest && !kv8_attention_plan(a).umma) return DART_ERR_INVALID_ARG;
   const int arch = check_arch();
   if (arch != DART_OK) return arch;
   const size_t layer = (size_t)in->layer * cache->n_pages * cache->n_kv_heads;

@@ -590,7 +590,7 @@ cudaError_t launch_stream_rows(const Kv8AttnArgs& a, const Kv8Plan& p, cudaStrea
 
 }  // namespace
 
-bool kv8_attention_many_rows(const Kv8AttnArgs& a) { return make_plan(a, nullptr).umma != 0; }
+Kv8Plan kv8_attention_plan(const Kv8AttnArgs& a) { return make_plan(a, nullptr); }
 size_t kv8_attention_workspace(const Kv8AttnArgs& a) { return make_plan(a, nullptr).bytes; }
 
 cudaError_t launch_kv8_attention(const Kv8AttnArgs& a, void* workspace, int spin, int withhold, cudaStream_t st) {
