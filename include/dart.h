@@ -485,7 +485,7 @@ int dart_selftest_kv8_wait(const dart_kv8_cache* cache, const dart_kv8_attn_in* 
  * new values that the call writes there, or the page's scale if the sequence already has rows in it and that is larger;
  * codes are x / s rounded to nearest even (exact division, one rounding).  A scale that grows re-rounds the page's
  * older codes to it.  Infinities become the largest code; NaN becomes e4m3's NaN, or 0 in int8.
- * A slot that appears twice in `slots` is written once (the first time) and reported.
+ * A slot that two entries with rows name is written once (the first time) and reported; an entry with n_append 0 claims no slot.
  */
 typedef struct dart_kv8_append_in {
   int32_t first_layer, n_layers;
@@ -532,7 +532,8 @@ int dart_kv8_fork(const dart_kv8_pages* pages, const int32_t* src, const int32_t
 /*
  * Makes positions seq_len .. seq_len + n_new[i] - 1 of the slots seqs[i] writable: missing pages are taken from the free
  * ones (lowest ids first, in list order), a page in that range that other slots share is replaced by a copy of all
- * layers (when every slot that shares it is listed, the last one keeps it).  seq_lens stay.  All or nothing: without
+ * layers (when every slot that shares it is listed, the last one keeps it).  An entry with n_new 0 asks for nothing and may name a
+ * slot again.  seq_lens stay.  All or nothing: without
  * enough free pages nothing changes and the status is DART_ERR_CAPACITY.  n: 1..1024.
  */
 int dart_kv8_reserve(const dart_kv8_pages* pages, const dart_kv8_cache* cache, const int32_t* seqs, const int32_t* n_new, int32_t n,

@@ -71,16 +71,16 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
   bool bad = slot < 0 || slot >= a.max_seqs || n < 0 || n > a.max_append;
   const int len = bad ? 0 : a.seq_lens[slot];
   if (len < 0 || (long long)len + n > (long long)a.max_pages * a.pt) bad = true;
-  if (a.slots != nullptr) {                        // a slot named before is skipped
+  if (n == 0 && !bad) return;                      // (and claims no slot: the padding of a batch)
+  if (a.slots != nullptr) {                        // a slot that an entry with rows named before is skipped
     bool twice = false;
-    for (int t = tid; t < b; t += TEAM) twice |= a.slots[t] == slot;
+    for (int t = tid; t < b; t += TEAM) twice |= a.slots[t] == slot && (a.n_append == nullptr || a.n_append[t] != 0);
     if (team_any<TEAM>(twice)) bad = true;
   }
   if (bad) {
     if (tid == 0) kv8_report(a.status, KV8_BAD_ARG);
     return;
   }
-  if (n == 0) return;
   const bf16* src = (is_v ? a.v_new : a.k_new) + (size_t)layer * a.layer_stride + (size_t)h * DH;
   // the page of column `col` and the rows that go there
   struct Unit { int page, lo, pieces; uint4 v[PIECES]; };

@@ -119,13 +119,14 @@ __global__ void __launch_bounds__(kPgThreads) kv8_reserve_plan_kernel(const Kv8P
   int* dst = ws + kPgHead;
   int *src = dst + p.n_pages, *slot = src + p.n_pages, *column = slot + p.n_pages;
   // the columns [lo, lo + width) that item tid wants to write
-  s_slot[tid] = tid < n ? seqs[tid] : -1;
+  const int m = tid < n ? n_new[tid] : 0;
+  s_slot[tid] = m != 0 ? seqs[tid] : -1;         // an entry without positions claims no slot
   __syncthreads();
   int width = 0, lo = 0;
   if (tid < n) {
-    const int s = s_slot[tid], m = n_new[tid];
+    const int s = m != 0 ? s_slot[tid] : seqs[tid];
     bool bad = s < 0 || s >= p.max_seqs || m < 0;
-    bad |= count_before(s_slot, tid, s) > 0;
+    bad |= m != 0 && count_before(s_slot, tid, s) > 0;
     const int len = bad ? 0 : p.seq_lens[s];
     if (len < 0 || (!bad && (long long)len + m > (long long)p.max_pages * p.pt)) bad = true;
     if (bad) kv8_report(status, KV8_BAD_ARG);
