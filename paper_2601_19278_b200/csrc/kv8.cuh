@@ -215,6 +215,7 @@ __device__ __forceinline__ void kv8_store_row(const Kv8AttnArgs& a, int b, int h
   const __nv_bfloat162 x = __floats2bfloat162_rn(on ? o.x * inv : 0.f, on ? o.y * inv : 0.f);
   const __nv_bfloat162 y = __floats2bfloat162_rn(on ? o.z * inv : 0.f, on ? o.w * inv : 0.f);
   bf16* dst = a.out + ((size_t)((long long)b * a.rows + i / a.G) * a.hq + h * a.G + i % a.G) * a.c.dh + c4 * 4;
+  DART_CHECK(i >= 0 && i < a.rows * a.G && b < a.batch && h < a.c.hkv && c4 * 4 < a.c.dh, a.status)
   *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
 }
 

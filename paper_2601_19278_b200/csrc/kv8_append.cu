@@ -167,6 +167,7 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
             if (FMT == KV8_INT8 && f[q] < -127.f) f[q] = -127.f;
           }
         }
+        DART_CHECK(x.lo >= 0 && x.lo * kPer + e < a.pt * kPer && layer < a.n_layers && h < a.hkv, a.status)
         *reinterpret_cast<uint2*>(codes + (size_t)x.lo * DH + (size_t)e * 8) =
             make_uint2(kv8_pack4<FMT>(f[0], f[1], f[2], f[3]), kv8_pack4<FMT>(f[4], f[5], f[6], f[7]));
       }
@@ -176,6 +177,7 @@ __global__ void __launch_bounds__(kApThreads) kv8_append_kernel(const __grid_con
       for (int e = tid; e < x.lo * DH / 4; e += TEAM) {
         uint32_t* c = reinterpret_cast<uint32_t*>(codes) + e;
         const uint32_t o = *c;
+        DART_CHECK(e * 4 < a.pt * DH, a.status)
         *c = kv8_pack4<FMT>(kv8_value<FMT>(o & 255) * ratio, kv8_value<FMT>((o >> 8) & 255) * ratio, kv8_value<FMT>((o >> 16) & 255) * ratio,
                             kv8_value<FMT>(o >> 24) * ratio);
       }

@@ -441,8 +441,10 @@ __global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_at
       kv8_store_row(a, b, h, i, i < Nv, L, c4, acc);
     } else {
       const size_t part = ((size_t)(b * a.c.hkv + h) * plan.max_chunks + chunk_id) * NR + i;
-      *reinterpret_cast<float4*>(plan.o_part + part * DH + c4 * 4) = acc;
-      if (c4 == 0) *reinterpret_cast<float2*>(plan.ml_part + part * 2) = make_float2(M, L);
+      DART_CHECK(i < NR && chunk_id < plan.max_chunks, a.status) {
+        *reinterpret_cast<float4*>(plan.o_part + part * DH + c4 * 4) = acc;
+        if (c4 == 0) *reinterpret_cast<float2*>(plan.ml_part + part * 2) = make_float2(M, L);
+      }
     }
   }
 }

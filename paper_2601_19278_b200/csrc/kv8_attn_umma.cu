@@ -765,11 +765,14 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
               const __nv_bfloat162 v2 = __floats2bfloat162_rn(o[2 * q], o[2 * q + 1]);
               w[q] = *reinterpret_cast<const uint32_t*>(&v2);
             }
+            DART_CHECK(r_out < a.rows && cb < DH, a.status)
             *reinterpret_cast<uint4*>(out + cb) = make_uint4(w[0], w[1], w[2], w[3]);
           } else {
             float4* dst = reinterpret_cast<float4*>(plan.o_part + part * DH + cb);
-            dst[0] = make_float4(o[0], o[1], o[2], o[3]);
-            dst[1] = make_float4(o[4], o[5], o[6], o[7]);
+            DART_CHECK(tile < plan.n_tiles && chunk_id < plan.max_chunks, a.status) {
+              dst[0] = make_float4(o[0], o[1], o[2], o[3]);
+              dst[1] = make_float4(o[4], o[5], o[6], o[7]);
+            }
           }
         }
         __syncwarp();

@@ -82,8 +82,10 @@ __global__ void __launch_bounds__(256) kv8_fork_kernel(const Kv8PagesArgs p, con
   for (int j = tid; j < cols; j += blockDim.x) {
     const int e = p.table[(size_t)s * p.max_pages + j];
     if (e < 0 || e >= p.n_pages) { kv8_report(status, KV8_BAD_ARG); continue; }
-    p.table[(size_t)d * p.max_pages + j] = e;
-    atomicAdd(&p.ref[e], 1);
+    DART_CHECK(d < p.max_seqs && j < p.max_pages, status) {
+      p.table[(size_t)d * p.max_pages + j] = e;
+      atomicAdd(&p.ref[e], 1);
+    }
   }
   if (tid == 0) p.seq_lens[d] = len;
 }
@@ -175,6 +177,7 @@ __global__ void __launch_bounds__(kPgThreads) kv8_reserve_plan_kernel(const Kv8P
     }
     int here;
     const int k = total_need + block_scan(need, sh, &here);
+    DART_CHECK(!need || (k >= 0 && k < p.n_pages), status)
     if (need) { src[k] = old; slot[k] = s; column[k] = j; }
     total_need += here;
   }
@@ -203,9 +206,11 @@ __global__ void __launch_bounds__(kPgThreads) kv8_reserve_plan_kernel(const Kv8P
   if (ok)
     for (int k = tid; k < total_need; k += kPgThreads) {
       const int page = dst[k];
-      p.table[(size_t)slot[k] * p.max_pages + column[k]] = page;
-      p.ref[page] = 1;
-      if (src[k] >= 0) atomicSub(&p.ref[src[k]], 1);
+      DART_CHECK(page >= 0 && page < p.n_pages && slot[k] >= 0 && slot[k] < p.max_seqs && column[k] >= 0 && column[k] < p.max_pages && src[k] < p.n_pages, status) {
+        p.table[(size_t)slot[k] * p.max_pages + column[k]] = page;
+        p.ref[page] = 1;
+        if (src[k] >= 0) atomicSub(&p.ref[src[k]], 1);
+      }
     }
   if (tid == 0) {
     ws[0] = ok ? total_need : 0;
@@ -213,7 +218,7 @@ __global__ void __launch_bounds__(kPgThreads) kv8_reserve_plan_kernel(const Kv8P
   }
 }
 
-__global__ void __launch_bounds__(kPgThreads) kv8_compact_plan_kernel(const Kv8PagesArgs p, int* ws, int* n_live_out) {
+__global__ void __launch_bounds__(kPgThreads) kv8_compact_plan_kernel(const Kv8PagesArgs p, int* ws, int* n_live_out, int* status) {
   __shared__ int sh[33];
   const int tid = threadIdx.x;
   pdl_wait();
@@ -240,8 +245,10 @@ __global__ void __launch_bounds__(kPgThreads) kv8_compact_plan_kernel(const Kv8P
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int id = base + tid * 4 + q;
-      if ((moves >> q) & 1) src[ks++] = id;
-      if ((holes >> q) & 1) dst[kd++] = id;
+      DART_CHECK(ks < p.n_pages && kd < p.n_pages, status) {
+        if ((moves >> q) & 1) src[ks++] = id;
+        if ((holes >> q) & 1) dst[kd++] = id;
+      }
     }
     n_src += here_src;
     n_dst += here_dst;
@@ -261,7 +268,8 @@ __global__ void __launch_bounds__(kPgThreads) kv8_compact_plan_kernel(const Kv8P
 
 // Copies the listed pages of every layer, and (compact) renames the table's entries.
 constexpr int kCpThreads = 256, kCpChunk = kCpThreads * 64;   // bytes a block copies at a time
-__global__ void __launch_bounds__(kCpThreads) kv8_copy_pages_kernel(const Kv8PagesArgs p, const Kv8PoolArgs c, const int* ws, int rename) {
+__global__ void __launch_bounds__(kCpThreads) kv8_copy_pages_kernel(const Kv8PagesArgs p, const Kv8PoolArgs c, const int* ws, int rename,
+                                                                     int* status) {
   pdl_wait();
   const int tid = threadIdx.x, count = ws[0];
   const int* dst = ws + kPgHead;
@@ -293,10 +301,16 @@ __global__ void __launch_bounds__(kCpThreads) kv8_copy_pages_kernel(const Kv8Pag
       if (at + q * kCpThreads < n16) v[q] = from[at + q * kCpThreads];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-      if (at + q * kCpThreads < n16) into[at + q * kCpThreads] = v[q];
+      if (at + q * kCpThreads < n16) {
+        DART_CHECK(d >= 0 && d < p.n_pages && layer < c.n_layers, status)
+        into[at + q * kCpThreads] = v[q];
+      }
     if (part == 0) {
       float* sc = is_v ? c.vs : c.ks;
-      for (int h = tid; h < c.hkv; h += kCpThreads) sc[dp * c.hkv + h] = sc[sp * c.hkv + h];
+      for (int h = tid; h < c.hkv; h += kCpThreads) {
+        DART_CHECK(d >= 0 && d < p.n_pages, status)
+        sc[dp * c.hkv + h] = sc[sp * c.hkv + h];
+      }
     }
   }
 }
@@ -332,14 +346,13 @@ cudaError_t launch_kv8_reserve(const Kv8PagesArgs& p, const Kv8PoolArgs& c, cons
                                cudaStream_t st) {
   const cudaError_t e = launch_ahead(kv8_reserve_plan_kernel, 1, kPgThreads, st, p, seqs, n_new, n, ws, status);
   if (e != cudaSuccess) return e;
-  return launch_ahead(kv8_copy_pages_kernel, kCpGrid, kCpThreads, st, p, c, ws, 0);
+  return launch_ahead(kv8_copy_pages_kernel, kCpGrid, kCpThreads, st, p, c, ws, 0, status);
 }
 
 cudaError_t launch_kv8_compact(const Kv8PagesArgs& p, const Kv8PoolArgs& c, int* n_live, int* ws, int* status, cudaStream_t st) {
-  (void)status;
-  const cudaError_t e = launch_ahead(kv8_compact_plan_kernel, 1, kPgThreads, st, p, ws, n_live);
+  const cudaError_t e = launch_ahead(kv8_compact_plan_kernel, 1, kPgThreads, st, p, ws, n_live, status);
   if (e != cudaSuccess) return e;
-  return launch_ahead(kv8_copy_pages_kernel, kCpGrid, kCpThreads, st, p, c, ws, 1);
+  return launch_ahead(kv8_copy_pages_kernel, kCpGrid, kCpThreads, st, p, c, ws, 1, status);
 }
 
 }  // namespace dart
