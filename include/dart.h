@@ -421,7 +421,7 @@ typedef struct dart_kv8_cache {
  * rows that see no key and rows from n_rows[b] on are zero.  Sums are fp32; weights enter the second product as fp16, relative to
  * what a key contributes (weight times value scale), so the scales of a sequence may lie far apart (a span of 2^90 is safe):
  * each is off by at most 2^-11 of itself or 2^-34 of the largest, whichever is more.  Queries and new rows enter the products
- * as fp16 multiples of a power of two near the row's largest element: elements below 2^-17 of it are off by up to 2^-25 of it.
+ * as fp16 multiples of a power of two near the row's largest element: elements below 2^-17 of it are off by up to 2^-25 of it (new values: 2^-23 and 2^-31).
  * What hidden rows, rows that do not exist and positions
  * behind a sequence's length hold (infinities and NaN included) does not reach the output.
  */

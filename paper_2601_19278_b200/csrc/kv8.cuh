@@ -162,6 +162,10 @@ __device__ __forceinline__ float kv8_pow2(int k) { return __uint_as_float((uint3
 __device__ __forceinline__ int kv8_row_exp(uint32_t bits) {
   return bits == 0u ? -64 : min(max((int)(bits >> 7) - 127, -100), 126);
 }
+// A new row's values become multiples of 2^(its exponent - kv8_lift): largest in [2^8, 2^9) or [2^6, 2^7), as a page's largest code
+// is, so that a new row weighs next to cached ones as much as it contributes.  (With the largest in [1, 2) every row's
+// reference moved at its first new key, 2^7 above the cached ones: prompt chunk 267 us.)
+constexpr __host__ __device__ int kv8_lift(int format) { return format == KV8_E4M3 ? 8 : 6; }
 // max of `big` and the eight |x| that are finite, as bf16 bits
 __device__ __forceinline__ uint32_t kv8_max_finite(uint32_t big, const uint4& v) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};

@@ -3,15 +3,16 @@
 //   out[r] = sum_y softmax_y(q[r] . k[y] / sqrt(d)) v[y],   k[y] = s_k * code,  v[y] = s_v * code
 //
 // Codes of both formats are exact in fp16, and so is a bf16 query or new row once divided by a power of two near its
-// largest element, but for elements below 2^-17 of that (off by up to 2^-25 of it): both products run on fp16 tensor-core
-// instructions with next to nothing rounded but the weights.  The scales
+// largest element, but for elements below 2^-17 of that (off by up to 2^-25 of it; new values 2^-23 and 2^-31, or less): both
+// products run on fp16 tensor-core instructions with next to nothing rounded but the weights.  The scales
 // never touch the codes: with c = log2(e) / sqrt(d) times the query's power of two, a key of a page with scales s_k, s_v
 // enters as
 //   x = (c s_k) (q . code) + log2(s_v),     P = 2^(x - m + 9),     2^9 l += P / s_v,     O += P code,     out = O / (2^9 l)
 // where m follows the largest x (not the largest score): P is the key's weight times its value's scale, 2^15 at most, so its
 // rounding to fp16 is 2^-11 of what the key contributes, however far apart the pages' scales are, or, for P below 2^-14, 2^-34 of
 // the largest weight times scale (kv8.cuh: kKv8Bias); over n keys that is at most n 2^-34 of the largest |v| on the
-// scale of the heaviest key's page.  m, l and O are fp32.  New rows are keys with a power-of-two scale of their own.
+// scale of the heaviest key's page.  m, l and O are fp32.  New rows are keys with a power-of-two scale of their own
+// (kv8.cuh: kv8_row_exp, kv8_lift).
 //
 // Rows of all query heads that share a KV head are one matrix (row r, head g of the group -> r * G + g).  Up to 24 such
 // rows (32 with d = 64: kv8_stream_rows) run on kv8_attn_stream_kernel below: a stream of the cache at memory speed.  More rows run on tcgen05
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(kStWarps * 32, kv8_stream_ctas(DH, NT)) kv8_at
       }
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, d));
-      ev[e] = kv8_row_exp(big);
+      ev[e] = kv8_row_exp(big) - kv8_lift(FMT);
 #pragma unroll
       for (int w = 0; w < DH / 64; ++w) {
         uint32_t f[4];

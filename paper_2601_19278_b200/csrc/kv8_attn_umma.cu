@@ -148,9 +148,9 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 // One bf16 row, divided by a power of two near its largest finite element, as row `row` of an fp16 operand tile.  Through
 // the row's own place in shared memory, in loops: code that runs once per CTA has to be short, because instructions that
 // are not in the cache cost far more than their work (unrolled, this and the epilogue took 30000 cycles of a 100000-cycle
-// CTA).  `odd`: values that are not finite become zero, and whether there were any is returned.
+// CTA).  The largest element ends up in [2^lift, 2^(lift + 1)).  `odd`: values that are not finite become zero, and whether there were any is returned.
 template <int DH>
-__device__ __forceinline__ bool ku_row_to_operand(const bf16* src, bool on, uint8_t* tile, int row, bool odd, float& inv, int& ex) {
+__device__ __forceinline__ bool ku_row_to_operand(const bf16* src, bool on, uint8_t* tile, int row, bool odd, int lift, int& ex) {
   const uint32_t base = smem_u32(tile) + row * 128;
   const int bytes = on ? 16 : 0;         // 0: zeros, nothing is read
 #pragma unroll 4
@@ -179,8 +179,8 @@ __device__ __forceinline__ bool ku_row_to_operand(const bf16* src, bool on, uint
       if (odd) { any |= kv8_zero_non_finite(w); *v = w; }
     }
   }
-  ex = kv8_row_exp(big);
-  inv = kv8_pow2(-ex);
+  ex = kv8_row_exp(big) - lift;
+  const float inv = kv8_pow2(-ex);
 #pragma unroll 2
   for (int c = 0; c < DH / 8; ++c) {
     uint4* v = reinterpret_cast<uint4*>(place + (c >> 3) * 16384 + (((c & 7) ^ (row & 7)) << 4));
@@ -459,9 +459,8 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
         const int y0 = (j0 + j - tl.cached) << 7, y = y0 + ct;
         const bool on = y < s.rows;
         const bf16* src = (is_v ? a.v_new : a.k_new) + (size_t)((long long)b * a.rows + (on ? y : 0)) * a.new_stride + (size_t)h * DH;
-        float inv;
         int ex;
-        const bool odd = ku_row_to_operand<DH>(src, on, tiles + buf * Ly::tile, ct, is_v != 0, inv, ex);
+        const bool odd = ku_row_to_operand<DH>(src, on, tiles + buf * Ly::tile, ct, is_v != 0, is_v ? kv8_lift(FMT) : 0, ex);
         if (is_v) {
           const uint32_t bits = __ballot_sync(0xffffffffu, odd);
           if (lane == 0 && bits != 0u) { s_bad[(y0 >> 5) + cw] = bits; sh.any_bad = 1; }
@@ -483,10 +482,9 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
     const uint32_t tS = tmem + ((uint32_t)(wq * 32) << 16) + p * 256, tO = tS + 128;
     float crow = 0.f;
     if (pair || p == 0) {
-      float inv;
       int ex;
       ku_row_to_operand<DH>(a.q + (on ? (size_t)((long long)b * a.rows + r) * a.q_stride + (size_t)(h * a.G + i_row - r * a.G) * DH : 0), on,
-                            sQ + (pair ? p : 0) * Ly::tile, row, false, inv, ex);
+                            sQ + (pair ? p : 0) * Ly::tile, row, false, 0, ex);
       crow = a.scale_log2e * kv8_pow2(ex);
       if (!pair) s_ml[0][row].x = crow;
       fence_async_smem();

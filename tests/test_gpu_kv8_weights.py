@@ -38,9 +38,9 @@ def exact(c, q, kn, vn, i, rows):
         k, v = (c.pool.read(w, 0, h, c.pages[i], c.lens[i]) for w in (0, 1))
         s = np.repeat([float(c.pool.scales[1][0, p, h]) for p in c.pages[i]], c.pt)[:c.lens[i]]
         new = [x[i, :, h].double().numpy() for x in (kn, vn)]
-        # a new row's scale is the power of two below its largest element
+        # a new row's scale puts its largest element where a page's largest code is
         top = np.abs(new[1]).max(1)
-        s_new = np.where(top > 0, 2.0 ** np.floor(np.log2(np.where(top > 0, top, 1.0))), 2.0 ** -64)
+        s_new = np.where(top > 0, 2.0 ** np.floor(np.log2(np.where(top > 0, top, 1.0))), 2.0 ** -64) * 2.0 ** (-8 if c.fmt == "e4m3" else -6)
         for j in range(h * (H // c.hkv), (h + 1) * (H // c.hkv)):
             for z, x in enumerate(rows):
                 ks, vs = np.concatenate([k, new[0][:x + 1]]), np.concatenate([v, new[1][:x + 1]])
