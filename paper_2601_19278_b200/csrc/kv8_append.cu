@@ -43,8 +43,8 @@ __device__ __forceinline__ float kv8_value(uint32_t code) {
 // and the units in flight have to fill the GPU: four per block of warp teams, and no more registers than the page size
 // asks for in a block team (PIECES 16-byte pieces per thread).  Next to the latencies it is instructions: a page's
 // largest value comes from 16-bit three-way maxima of the raw words, rows are found by adding a stride.
-// Measured: 16 accepted paths x 16 layers x 8 heads (8.3 MB) 7.1 us, 39 with a block of 256 per unit; 4 x 2047 prompt rows x
-// 8 heads (50 MB) 13.4 us = 0.57 of the copy peak, 35 with the rows read after the page, 20 with element-wise maxima, 14.9
+// Measured (device time, back to back in a CUDA graph; through Python 8.2 and 14.5): 16 accepted paths x 16 layers x 8 heads (8.3 MB)
+// 7.2 us, 39 with a block of 256 per unit; 4 x 2047 prompt rows x 8 heads (50 MB) 13.75 us = 0.56 of the copy peak, 35 with the rows read after the page, 20 with element-wise maxima, 14.9
 // in blocks of 256, 19 in warp teams; strips of pages per block, the next page's rows in flight: 32.
 constexpr int kApThreads = 128;
 

@@ -72,9 +72,10 @@ constexpr __host__ __device__ int st_body() {
 
 // NT tiles of 8 rows.  With more of them the instructions per byte grow and registers run out (O and Q take 48 NT a thread at
 // d = 128, 24 NT at 64), which sets how many CTAs fit an SM; tcgen05 converts a step's codes at one cost for 1 to 128 rows.
-// Both sides, 8 KV heads, e4m3, us here and there: 16 sequences of 8192 keys, d = 128: 20 rows 87, 107; 32 rows 148
-// (spilled), 107; d = 64: 24 rows 63, 91; 32 rows 72, 91.  64 of 2048, d = 128: 20 rows 101, 146; d = 64: 32 rows 87, 122.
-// A single sequence of 8192 loses: d = 128, 20 rows 18.4, 17.4; d = 64, 32 rows 16.6, 15.3.
+// Both sides, 8 KV heads, e4m3, us here and there: 16 sequences of 8192 keys, d = 128: 4 rows x 5 heads 88, 109; 32 rows 148
+// (spilled), 110; d = 64: 6 x 4 61, 93; 8 x 4 72.5, 94.  64 of 2048, d = 128: 4 x 5 101, 148; d = 64: 8 x 4 86.5, 123.  New rows are
+// the last warp's own, 16 at a time: 20 rows of one head 93, 110.  A single sequence of 8192 loses: d = 128, 4 x 5 18.7, 17.6, 20
+// of one head 22.6, 17.7; d = 64, 8 x 4 16.4, 15.4.
 // d = 64, 64 sequences of 2048 keys: four CTAs to an SM instead of three for 8 rows 37 us, 41; three instead of two for 16 rows
 // 50, 57.
 constexpr __host__ __device__ int kv8_stream_ctas(int dh, int nt) { return nt == 1 ? (dh == 64 ? 4 : 3) : nt == 2 && dh == 64 ? 3 : 2; }
@@ -536,8 +537,11 @@ namespace {
 
 // Keys a CTA of the streaming kernel takes.  With few (batch entry, KV head) pairs one wave of CTAs shares the
 // longest sequence evenly; with many, whose lengths differ in a way only the device knows, two waves of shorter parts even
-// them out (64 ragged sequences: one wave 98.1 us, two 99.8, four 101.7, six 106.7).  At least 512 keys, so that a CTA's
-// start (page ids, queries, the join) stays a small part.
+// them out.  (One wave / two / four, us, 64 sequences of 512 to 8192 keys, longest first: 100.6 / 96.9 / 101.0, shortest first
+// 107 / 103 / 103, shuffled 106 / 104 / 103; all of 4352: 123 / 110.5 / 106.5; 16 of 8192: 66 / 59 / 61; one of 16384 among 63 of
+// 1024: 95 / 94 / 66.)  All of it by max_len, not by the lengths, so a loose bound costs: 64 sequences with a bound of four times
+// the longest 97 -> 101.6, one of 4096 keys with a bound of 131072 12.2 -> 21.1.  At least 512 keys, so that a CTA's start (page
+// ids, queries, the join) stays a small part.
 constexpr int kStMinChunk = 512, kStMaxChunk = 8192;
 int round128(long long x) { return (int)((x + 127) / 128 * 128); }
 

@@ -25,7 +25,7 @@
 // unrolled, it was 100 KB and each CTA waited for its instructions.
 // New rows are read by the converters themselves, each key divided by its own power of two; a value that is not finite is
 // kept out of the product (0 weight times NaN would reach rows that do not see it) and added at the end to the rows that do.
-// Every wait is bounded.
+// Every wait is bounded.  At the 96 registers of the launch the compiler spills 40 to 56 bytes a thread (192 to 204 bytes of loads).
 #include "kv8.cuh"
 #include "umma.cuh"
 #include "umma_attn.cuh"
@@ -42,9 +42,9 @@ constexpr int kKuBad = 4096 / 32;
 // 2600 cycles (measured), which leaves the issue slots to the softmax warps beside it (1 % of the kernel's time against
 // test_wait, with or without a pause between two looks; with a suspend-time hint, or a look at the clock, 2 to 3 % slower).
 // `patience`, in shared memory, is how many tries every wait of the CTA has (plan.spin); the wait that runs out sets it to 0 and
-// all roles leave.  (As an argument of the kernel the limit took a register that the softmax warps do not have: 16 trees 178 us,
-// the prompt chunk 287, here 174.5 and 267.)  A whole warp waits and one answer is every lane's, since what follows has
-// instructions that all lanes have to meet; the votes take no time that shows.
+// all roles leave.  (As an argument of the kernel the limit took a register that the softmax warps do not have: 2 % of 16
+// trees, 7 % of the prompt chunk.)  A whole warp waits and one answer is every lane's, since what follows has
+// instructions that all lanes have to meet; the votes take 0.2 %.
 __device__ __forceinline__ bool ku_wait(uint64_t* bar, uint32_t parity, volatile int* patience) {
 #pragma unroll 1
   for (int it = 0;; ++it) {
@@ -803,11 +803,12 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
 
 // Key steps of a CTA.  A CTA's start and end (queries, the first copies, the first scores, its result) cost as much as five or
 // six steps, and a partial result is written, read again and joined, so the keys are split only as far as one wave of
-// CTAs, one to an SM, goes.  (Measured, steps per CTA: 16 ragged sequences of up to 65 steps, 256 cells: 65 steps 169 us, 33: 192,
-// 16: 226; prompt chunk, 256 cells of 44: 44 steps 291 us, 22: 353; one tree in pairs, 16 cells of 33 steps: 4 steps 32 us, 3: 37, 8: 38.)
+// CTAs, one to an SM, goes.  (Measured, steps per CTA: 16 ragged sequences of up to 65 steps, 256 cells: 65 steps 175 us, 33: 203,
+// 16: 238; prompt chunk, 256 cells of 44: 44 steps 247 us, 22: 316; one tree in pairs, 16 cells of 33 steps: 4 steps 32.4 us, 3: 35.5, 8:
+// 37.6.)  By max_len, not by the lengths: one tree over 4096 keys 27 us with that bound, 65 with 32768, 97 with 131072.
 // A step of two row tiles takes about 2.2 us and the CTA around it 15; a step of one tile 1.6 us and its CTA 11: two tiles
 // are cheaper by the row, one tile is done sooner where the GPU is not full anyway (one tree over 33 steps,
-// 3 tiles of 8 heads: 28.4 us in single tiles, 31.9 in pairs).
+// 3 tiles of 8 heads: 27.0 us in single tiles, 32.4 in pairs).
 void kv8_umma_plan(const Kv8AttnArgs& a, Kv8Plan& p) {
   constexpr int kSms = 148, kMinSteps = 4;
   p.n_tiles = (a.rows * a.G + 127) / 128;

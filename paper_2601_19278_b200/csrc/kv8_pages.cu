@@ -6,8 +6,9 @@
 // (source, destination) pages in the workspace, and a copy kernel over the list, whose length only the device knows.  The
 // copies run at memory speed (48 pages of 16 layers, 200 MB read and written: 27 us); what the small kernels before them
 // cost is their launches and chains of dependent reads, so every kernel here is launched ahead of its predecessor's end
-// (pdl_wait) and the planning kernels compare lists in shared memory.  Measured, with the restoring of the
-// tables between two passes (2 us): 16 sequences forked three times, then all 64 reserved, 40.9 us; one fork and reserve of a
+// (pdl_wait) and the planning kernels compare lists in shared memory.  Measured (device time, back to back in a CUDA
+// graph; through Python 44, 18 and 146), with the restoring of the tables between two passes (2 us): 16 sequences forked three
+// times, then all 64 reserved, 40.8 us; one fork and reserve of a
 // short sequence 9.8 us; compaction after releasing half of 64 sequences (169 pages of 16 layers, 709 MB) 137 us, the
 // copies alone 122 = 0.89 of the copy peak.
 #include "kv8.cuh"
