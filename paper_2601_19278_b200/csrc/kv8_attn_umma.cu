@@ -25,7 +25,7 @@
 // unrolled, it was 100 KB and each CTA waited for its instructions.
 // New rows are read by the converters themselves, each key divided by its own power of two; a value that is not finite is
 // kept out of the product (0 weight times NaN would reach rows that do not see it) and added at the end to the rows that do.
-// Every wait is bounded.  At the 96 registers of the launch the compiler spills 24 to 80 bytes a thread (140 to 456 bytes of loads; the most for windows).
+// Every wait is bounded.  At the 96 registers of the launch the compiler spills 24 to 72 bytes a thread (140 to 440 bytes of loads; the most for windows).
 #include "kv8.cuh"
 #include "umma.cuh"
 #include "umma_attn.cuh"
@@ -621,6 +621,9 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       // WIN: the half step's first position, and whether every row of the warp has all 64 in its window or among the sinks
       const int k_pos = (cached ? step << 7 : s.len + ((step - tl.cached) << 7)) + hf * 64;
       const bool inside = !WIN || k_pos >= lo_top || k_pos + 64 <= a.sinks;
+      // What scores are multiplied by.  WIN: hidden ones are -infinity already, and a query's size times a key's scale may underflow (a query of zeros
+      // counts as 2^-64, scales go down to 2^-100): the smallest normal number makes as little of finite scores, and -infinity of infinite ones.
+      auto factor = [&](float key) { return WIN ? fmaxf(crow * key, kv8_pow2(-126)) : crow * key; };
       // a new reference maximum rescales what O holds, once the half step before has been added to it
       auto raise = [&](float mt, float rise) -> bool {
         float alpha = 1.f;
@@ -645,8 +648,10 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
         }
         return true;
       };
-      // New rows in one pass against the reference so far, a scale per key; false: a weight was too large, nothing is written.
+      // New rows in one pass against the reference so far, a scale per key; false: a weight was too large (or, WIN, a hidden score's factor nothing),
+      // nothing is written.  A row that sees none of them takes 1 for its query's size: keys' scales are 2^-100 or more, so its weights are zero.
       auto new_rows_pass = [&](bool sees_some) -> bool {
+        const float by = WIN && !sees_some ? 1.f : crow;
         const float mu = m_ref == -INFINITY ? 0.f : m_ref - kKv8Bias;
         float w0 = 0.f, w1 = 0.f;
         uint32_t pk[32];
@@ -658,8 +663,8 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
 #pragma unroll
           for (int q = 0; q < 16; q += 2) {
             const float4 c = *reinterpret_cast<const float4*>(scp + c0 + q);      // two keys
-            const float p0 = kv8_ex2(fmaf(__uint_as_float(rr[q]), crow * c.x, c.y - mu));
-            const float p1 = kv8_ex2(fmaf(__uint_as_float(rr[q + 1]), crow * c.z, c.w - mu));
+            const float p0 = kv8_ex2(fmaf(__uint_as_float(rr[q]), by * c.x, c.y - mu));
+            const float p1 = kv8_ex2(fmaf(__uint_as_float(rr[q + 1]), by * c.z, c.w - mu));
             w0 = fmaf(p0, kv8_ex2(-c.y), w0);
             w1 = fmaf(p1, kv8_ex2(-c.w), w1);
             const __half2 v2 = __floats2half2_rn(p0, p1);
@@ -728,7 +733,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
               float x0 = __uint_as_float(rr[0]);
 #pragma unroll
               for (int q = 1; q < 15; q += 2) x0 = max3(x0, __uint_as_float(rr[q]), __uint_as_float(rr[q + 1]));
-              mt = fmaxf(mt, fmaf(fmaxf(x0, __uint_as_float(rr[15])), crow * c.x, c.y));
+              mt = fmaxf(mt, fmaf(fmaxf(x0, __uint_as_float(rr[15])), factor(c.x), c.y));
             }
             ok = raise(mt, 0.5f);
             if (!ok) break;
@@ -744,7 +749,7 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
               const float2 c = scp[g * 16];
-              const float mul = crow * c.x, sub = c.y - mu;
+              const float mul = factor(c.x), sub = c.y - mu;
               const f32x2 mul2 = pack2(mul, mul), sub2 = pack2(sub, sub);
 #pragma unroll
               for (int q = 0; q < 16; q += 2)
