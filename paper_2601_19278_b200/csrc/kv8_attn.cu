@@ -631,7 +631,6 @@ Kv8Plan make_plan(const Kv8AttnArgs& a, void* workspace) {
     most = (size_t)pairs * part * (size_t)(by_min < bound ? by_min : bound);
     rows = (size_t)pairs * part * p.max_chunks;
     if (longest_len <= kStMinChunk) most = 0;
-    if (most < rows) most = rows;        // (uneven parts: of any length)
   } else {
     kv8_umma_plan(a, p);
     rows = (size_t)a.batch * a.c.hkv * p.n_tiles * 128 * p.max_chunks;
