@@ -620,9 +620,13 @@ Kv8Plan make_plan(const Kv8AttnArgs& a, void* workspace) {
     // Where a window makes the lengths alike, equal parts start and end together: the SMs' copies pause together, and the last wave is mostly
     // empty.  Parts of sizes that differ from pair to pair, the larger ones first, do neither.  (64 sequences with 4100 keys in their
     // windows, 8 KV heads, floor 77.8 us: two equal parts 105.5, three to six 102 to 105; a half, a quarter and two eighths 101.4; a first part
-    // of 10 to 22 32nds 97.5, of 14 to 30 95.1.)  With fewer pairs than half a wave one wave takes all; over four waves it evens out by itself.
+    // of 10 to 22 32nds 97.5, of 14 to 30 95.1.)  They gain with about a wave of pairs (two to five head layouts and windows of 1100 to 4096 each, sequences
+    // all of 8192 keys and from an eighth of the window on, equal parts' time over theirs: 0.75 of a wave 1.08, 0.85 1.07, 1.0 1.03, 1.3 1.01).  With more
+    // pairs equal parts are as good and then better: 1.5 waves 0.98, 2 0.93, 3 0.90.  With fewer, a first part can take longer than
+    // the whole call in equal ones, which are many there, unless those are short anyway (half a wave: 1100 keys 0.99, 2000 1.06, 4096 0.79).
     const int part32 = (int)((longest_len + 511ll) / 512 * 16), first = (kKv8FirstLeast + kKv8FirstKinds - 1) * part32;
-    p.uneven = longest_len < a.max_len && pairs * 2 > slots && pairs < 4 * slots && longest_len > 2 * kStMinChunk && first <= kStMaxChunk;
+    p.uneven = longest_len < a.max_len && pairs * 2 > slots && pairs * 3 < 4 * slots && (pairs * 4 > 3 * slots || longest_len <= 5 * kStMinChunk) &&
+               longest_len > 2 * kStMinChunk && first <= kStMaxChunk;
     if (p.uneven) p.chunk = first;
     p.max_chunks = p.uneven ? 3 : kv8_split(longest_len, p.chunk, 128).n;
     p.n_tiles = 1;
