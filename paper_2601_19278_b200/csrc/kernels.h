@@ -47,10 +47,10 @@ int check_sm100();
 // Launch with programmatic stream serialization (see pdl_wait / pdl_trigger in common.cuh).  launch_ahead leaves the shared-memory
 // carve-out alone, for kernels that live on L1 (with the largest carve-out page copies took 138 us instead of 123).
 template <class... KArgs, class... Args>
-inline cudaError_t launch_ahead(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t st, Args&&... args) {
+inline cudaError_t launch_ahead(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
-  cfg.blockDim = dim3(block);
+  cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
@@ -63,7 +63,7 @@ inline cudaError_t launch_ahead(void (*kernel)(KArgs...), dim3 grid, int block, 
 template <class... KArgs, class... Args>
 inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
   prefer_max_shared(reinterpret_cast<const void*>(kernel));
-  return launch_ahead(kernel, grid, (int)block.x, smem, st, static_cast<Args&&>(args)...);
+  return launch_ahead(kernel, grid, block, smem, st, static_cast<Args&&>(args)...);
 }
 
 // ---------------------------------------------------------------------------------------------
