@@ -621,6 +621,9 @@ size_t dart_kv8_attention_window_workspace_bytes(const dart_kv8_cache* cache, in
 /* How such a call is cut, as dart_kv8_attention_plan tells it: by max_len or the window, whichever is less. */
 int dart_kv8_attention_window_plan(const dart_kv8_cache* cache, int32_t batch, int32_t rows, int32_t n_q_heads, int32_t max_len, int32_t window,
                                    int32_t sinks, int32_t with_new_rows, dart_kv8_plan* out);
+/* dart_selftest_kv8_wait of such a call: the kernel's instances with a window wait for the new rows' tiles as well. */
+int dart_selftest_kv8_window_wait(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, const dart_kv8_window* window, int32_t spin_limit,
+                                  int32_t missing_from, void* cuda_stream);
 /*
  * The slots give back the pages that lie wholly behind the window of every row to come (positions <= seq_len - window) and hold no sink
  * (positions >= sinks); their table entries become DART_KV8_GIVEN_BACK, the other slots that share them keep them.  For pools whose layers all attend to

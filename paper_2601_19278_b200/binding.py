@@ -31,7 +31,7 @@ EXPORTS = [
     "dart_last_cuda_error", "dart_status_string", "dart_workspace_bytes", "dart_ngram_bytes", "dart_train_attention_fwd", "dart_step_launch_count", "dart_draft_prefill", "dart_tree_verify_inputs",
     "dart_set_profile_events", "dart_topk_rows_noalloc", "dart_selftest_bounded_wait", "dart_draft_step_host",
     "dart_kv8_attention", "dart_kv8_attention_workspace_bytes", "dart_kv8_append", "dart_kv8_append_owned", "dart_kv8_fork", "dart_kv8_reserve", "dart_kv8_release",
-    "dart_kv8_compact", "dart_kv8_pages_workspace_bytes", "dart_selftest_kv8_wait",
+    "dart_kv8_compact", "dart_kv8_pages_workspace_bytes", "dart_selftest_kv8_wait", "dart_selftest_kv8_window_wait",
     "dart_kv8_attention_plan", "dart_kv8_attention_window", "dart_kv8_attention_window_workspace_bytes", "dart_kv8_attention_window_plan",
     "dart_kv8_trim", "dart_rope_frequencies", "dart_qk_norm_rope", "dart_token_logprobs", "dart_token_logprobs_workspace_bytes",
 ]
@@ -243,6 +243,8 @@ def lib() -> C.CDLL:
         L.dart_kv8_pages_workspace_bytes.argtypes = [P]
         L.dart_selftest_kv8_wait.argtypes = [P, P, C.c_int32, C.c_int32, P]
         L.dart_selftest_kv8_wait.restype = C.c_int
+        L.dart_selftest_kv8_window_wait.argtypes = [P, P, P, C.c_int32, C.c_int32, P]
+        L.dart_selftest_kv8_window_wait.restype = C.c_int
         for name in ("attention", "append", "append_owned", "fork", "release", "reserve", "compact"):
             getattr(L, "dart_kv8_" + name).restype = C.c_int
         L.dart_kv8_attention_workspace_bytes.restype = L.dart_kv8_pages_workspace_bytes.restype = C.c_size_t

@@ -155,9 +155,19 @@ int dart_kv8_attention_window(const dart_kv8_cache* cache, const dart_kv8_attn_i
   return attention(cache, in, window, false, kKv8Spin, -1, cuda_stream);
 }
 
-int dart_selftest_kv8_wait(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, int32_t spin_limit, int32_t missing_from, void* cuda_stream) {
+static int selftest(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, const dart_kv8_window* w, int spin_limit, int missing_from, void* cuda_stream) {
   if (in == nullptr || in->status == nullptr || spin_limit < 1 || spin_limit > 100000 || missing_from < 0) return DART_ERR_INVALID_ARG;
-  return attention(cache, in, nullptr, true, spin_limit, missing_from, cuda_stream);
+  return attention(cache, in, w, true, spin_limit, missing_from, cuda_stream);
+}
+
+int dart_selftest_kv8_wait(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, int32_t spin_limit, int32_t missing_from, void* cuda_stream) {
+  return selftest(cache, in, nullptr, spin_limit, missing_from, cuda_stream);
+}
+
+int dart_selftest_kv8_window_wait(const dart_kv8_cache* cache, const dart_kv8_attn_in* in, const dart_kv8_window* window, int32_t spin_limit,
+                                  int32_t missing_from, void* cuda_stream) {
+  if (window == nullptr) return DART_ERR_INVALID_ARG;
+  return selftest(cache, in, window, spin_limit, missing_from, cuda_stream);
 }
 
 static int append(const dart_kv8_cache* cache, const dart_kv8_append_in* in, const int32_t* ref, void* cuda_stream) {
