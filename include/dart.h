@@ -562,7 +562,8 @@ size_t dart_kv8_pages_workspace_bytes(const dart_kv8_pages* pages);
 /*
  * Frequencies for dart_qk_norm_rope: inv_freq (HOST, n of them, radians per position, |f| <= pi; rope_theta^(-2i / rotary_dim), or
  * any scaled form of it) as turns per position in 64-bit fractions (out, HOST), which the caller copies to the device once.
- * Angles are then exact modulo a turn at every position below 2^31.  Errors: INVALID_ARG (NULL, n outside 1..64, a frequency out of range).
+ * An angle modulo a turn is then off by at most 2^-26 of a turn (9.4e-8 radians) at every position below 2^31.  Errors: INVALID_ARG (NULL, n outside
+ * 1..64, a frequency out of range).
  */
 int dart_rope_frequencies(const double* inv_freq, int32_t n, uint64_t* out);
 /*

@@ -25,7 +25,7 @@
 // unrolled, it was 100 KB and each CTA waited for its instructions.
 // New rows are read by the converters themselves, each key divided by its own power of two; a value that is not finite is
 // kept out of the product (0 weight times NaN would reach rows that do not see it) and added at the end to the rows that do.
-// Every wait is bounded.  At the 96 registers of the launch the compiler spills 24 to 72 bytes a thread (140 to 440 bytes of loads; the most for windows).
+// Every wait is bounded.  At the 96 registers of the launch the compiler spills 24 to 72 bytes a thread (140 to 452 bytes of loads; the most for windows).
 #include "kv8.cuh"
 #include "umma.cuh"
 #include "umma_attn.cuh"

@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(256) kv8_release_kernel(const Kv8PagesArgs p, 
 
 // Columns [sinks / pt rounded up, (len - window + 1) / pt) lie behind the window of every row to come and hold no sink.  A block takes
 // kTrimCols columns of a slot at a time.  What bounds it is a launch and a chain of dependent reads (slot, length, entry, count), so the
-// entries of a thread are read together: 64 slots with 250000 entries 26.5 us with one block to a slot and one entry after the other, 7.1 so
+// entries of a thread are read together: 64 slots with 250000 entries 26.5 us with one block to a slot and one entry after the other, 7.3 so
 // (2 of them the restoring of the tables between two calls).
 constexpr int kTrimEach = 4, kTrimCols = 256 * kTrimEach;
 __global__ void __launch_bounds__(256) kv8_trim_kernel(const Kv8PagesArgs p, const int* seqs, int window, int sinks, int* status) {

@@ -5,12 +5,12 @@
 // per head, in fp32, with one rounding at the end; pairs (a, b) are (i, i + n/2) or neighbours (2i, 2i + 1) of the first n
 // elements, the rest of the head is not rotated.  Angles run to 10^5 and more radians, where an fp32 product has lost them
 // (2^-24 of 131072 is 0.008): frequencies are turns per position as 64-bit fractions, so that position * f wraps by itself and
-// leaves the angle to 2^-32 of a turn (dart_rope_frequencies).
+// has the angle to 2^-32 of a turn (dart_rope_frequencies); as an fp32 number of half turns it is off by up to 2^-26 of a turn, at any position.
 //
 // What bounds it is the bytes, each read and written once.  A head is 16 elements to a lane (two 8-element chunks that are each
 // other's partners, so that a pair never crosses lanes): 128-byte segments, four or eight heads to a warp, and a sum over
 // d / 16 lanes.  A block takes one token; its d / 2 sines are computed once for all heads, behind the loads of the heads.
-// 8191 rows of 48 bf16 heads of 128 out of a QKV matrix: 34.5 us = 5.8 TB/s, 0.89 of the copy peak (a plain copy of as much 33.2); one
+// 8191 rows of 48 bf16 heads of 128 out of a QKV matrix: 34.8 us = 5.8 TB/s, 0.88 of the copy peak (a plain copy of as much 33.2); one
 // operation to an instruction 37.5; more or fewer registers (6 to 8 blocks to an SM), 64 threads to a block and streaming stores change nothing,
 // 256 threads take 50.
 #include <cuda_fp16.h>
