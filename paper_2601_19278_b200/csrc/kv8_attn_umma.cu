@@ -623,7 +623,10 @@ __global__ void __launch_bounds__(kKuThreads, 1) kv8_attn_umma_kernel(const __gr
       const bool inside = !WIN || k_pos >= lo_top || k_pos + 64 <= a.sinks;
       // What scores are multiplied by.  WIN: hidden ones are -infinity already, and a query's size times a key's scale may underflow (a query of zeros
       // counts as 2^-64, scales go down to 2^-100): the smallest normal number makes as little of finite scores, and -infinity of infinite ones.
-      auto factor = [&](float key) { return WIN ? fmaxf(crow * key, kv8_pow2(-126)) : crow * key; };
+      auto factor = [&](float key) {
+        const float f = crow * key;
+        return WIN && f < kv8_pow2(-126) ? kv8_pow2(-126) : f;       // (a scale that is NaN stays one)
+      };
       // a new reference maximum rescales what O holds, once the half step before has been added to it
       auto raise = [&](float mt, float rise) -> bool {
         float alpha = 1.f;

@@ -31,3 +31,19 @@ def test_zero_and_tiny_queries_over_small_keys(fmt, R, H, tree, key_exp, query, 
     got = windowed(c, q, kn, vn, 1000, window, sinks, **kw)
     assert bool(torch.isfinite(got).all())
     check(c, got, q, kn, vn, window, sinks, only=None if tree else [0, 1, 2, 63, 64, 65, 88, 89, 90, 91, 92, 127, 128, R - 2, R - 1], **kw)
+
+
+@pytest.mark.parametrize("R,H,tree", [(1, 5, False), (60, 5, True), (300, 4, False)])
+def test_a_scale_that_is_nan_is_not_taken_for_a_small_one(R, H, tree):
+    """Such a page is a fault of the caller's; the rows that see it say so, whatever the number of rows, and the other sequences are unharmed."""
+    lens = [1000, 333]
+    c = Case(lens, 16, "int8", 1, 128, seed=R)
+    q, kn, vn = c.bf16(2, R, H, 128), c.bf16(2, R, 1, 128), c.bf16(2, R, 1, 128)
+    kw = {}
+    if tree:
+        mask, pos = trees(c.rng, lens, R, [R] * 2)
+        kw = dict(mask=mask, positions=pos)
+    c.t[2][0, c.pages[0][980 // 16]] = float("nan")
+    got = windowed(c, q, kn, vn, 1000, 150, 4, **kw)
+    sees = R if tree else min(R, 980 // 16 * 16 + 15 - 1000 + 150)      # the page's last position is in the window of so many rows
+    assert bool(got[0, :sees].isnan().all()) and bool(got[1].isfinite().all())
